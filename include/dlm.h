@@ -419,6 +419,108 @@ int dlm_window_qkv_project_stage(dlm_ctx* ctx, const void* x, const void* w, con
                                  void* v_out, const dlm_kv_cache* cache, int layer, void* workspace,
                                  size_t workspace_bytes, void* stream);
 
+/*
+ * The cache in 4 bits.  Rows are quantised when they are committed and stay so; queries, fresh rows and outputs stay bf16.
+ * (The paper keeps its cache in 16 bits; this is the same cache at 4.25 bits a value.)
+ *
+ * A row is groups of 32 consecutive values with one scale byte each.  Value = (n - 8) * s:
+ *   s  from the byte eeeeemmm: (1 + m / 8) * 2^(e - 20), 2^-20 .. 3840
+ *   n  1 .. 15; eight consecutive values are a little-endian 32-bit word, value j in bits 4 (j / 2) .. + 3 of its lower
+ *      16 bits (j even) or of its upper ones (j odd)
+ * dlm_kv_cache_commit_q4 takes for s the group's largest magnitude / 7, rounded to 4 significant bits (to nearest, ties to
+ * even) and clamped to the scale's range, and for n - 8 the quotient value / s rounded to the nearest integer, ties to even:
+ * no value within the range is off by more than s / 2.  Magnitudes above 26880 (7 * 3840), infinities among them, are stored as 26880, and a NaN as 0.
+ * Every value that a row can hold is exact in bf16.
+ *
+ *   k, v              device, uint8 [n_layers][batch][n_kv_heads][capacity][head_dim / 2]
+ *   k_scale, v_scale  device, uint8 [n_layers][batch][n_kv_heads][capacity][head_dim / 32]
+ *   cache_len         device, int32 [batch], as for dlm_kv_cache
+ * Supported: head_dim in {64, 128}, capacity a multiple of 8, k, v, k_scale and v_scale on 16 bytes (else
+ * DLM_ERR_UNSUPPORTED).  Rows at or beyond cache_len[b] never influence a result.
+ */
+typedef struct {
+  void* k;
+  void* v;
+  void* k_scale;
+  void* v_scale;
+  int32_t* cache_len;
+  int32_t n_layers, batch, n_kv_heads, capacity, head_dim;
+} dlm_kv_cache_q4;
+
+/* dlm_kv_cache_commit_q4 — dlm_kv_cache_commit into a 4-bit cache: the same rows to the same places, quantised.  Arguments, errors
+ * and data-dependent behaviour as there; of a destination given twice each of the pieces that may mix is 8 values or a scale. */
+int dlm_kv_cache_commit_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* cache, const void* k_new,
+                           const void* v_new, int src_len, const int32_t* src_idx,
+                           const int32_t* dst_pos, int dst_mode, const int32_t* n_rows, int n_max,
+                           int advance_len, int layer_begin, int layer_end, void* stream);
+
+/*
+ * dlm_kv_cache_read_q4 — rows of a 4-bit cache as bf16 (the values they hold; no rounding): to move a sequence to a cache of 16 bits
+ * or to another program.  For layer l of [layer_begin, layer_end), batch element b, r < n(b) and KV head:
+ *     out[l - layer_begin][b][head][r][:] = cache[l][b][head][src_pos ? src_pos[b * n_max + r] : r][:]
+ *   src_pos       device, int32 [batch][n_max] or NULL (then n_max <= capacity, else DLM_ERR_SHAPE)
+ *   n_rows        device, int32 [batch] or NULL; n(b) = n_rows ? n_rows[b] : n_max
+ *   k_out, v_out  device, bf16 [layer_end - layer_begin][batch][n_kv_heads][n_max][head_dim]; rows at or beyond n(b) are left as they were
+ * Any row of the capacity may be read; cache_len is not looked at.
+ * Data-dependent: n(b) outside [0, n_max]: nothing is written for b, DLM_ERR_CAPACITY; a position outside [0, capacity): that row is
+ * skipped, DLM_ERR_INDEX.
+ */
+int dlm_kv_cache_read_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* cache, const int32_t* src_pos, const int32_t* n_rows,
+                         int n_max, int layer_begin, int layer_end, void* k_out, void* v_out, void* stream);
+
+/* dlm_freecache_attn_step_q4 — dlm_freecache_attn_step over a 4-bit cache: keys and values are the cache's values and the fresh bf16
+ * rows.  Arguments, results, limits and data-dependent behaviour as there (cache_len_hint is not needed for correctness here either);
+ * the workspace is dlm_attn_workspace_bytes_q4's. */
+size_t dlm_attn_workspace_bytes_q4(const dlm_ctx* ctx, const dlm_kv_cache_q4* cache, int n_layers_in_call, int n_q_heads, int q_cap);
+int dlm_freecache_attn_step_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* cache, int layer_begin,
+                               int layer_end, const void* q, const void* k_new, const void* v_new,
+                               int n_q_heads, int q_cap, const int32_t* q_len, float softmax_scale,
+                               int cache_len_hint, void* out, float* lse, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+/*
+ * dlm_cache_weight_accumulate, dlm_cache_weight_accumulate_q4 — how much attention each cached row gets: after an attention step,
+ * for every layer l of [layer_begin, layer_end), batch element b, KV head g and cached row j < cache_len[b]
+ *     weight[l][b][g][j] = decay * collected[l][b][g][j] + sum_{h of g's query heads} sum_{i < q_len(b)} exp(scale * <q_hi, k_j> - lse_hi)
+ * with lse as that step wrote it (rows that are inactive there have lse = -inf and are left out here).  Products of bf16 values and
+ * sums in fp32.
+ *   q         device, bf16 [layers][batch][n_q_heads][q_cap][head_dim], the step's queries;  lse device, fp32 [layers][batch][n_q_heads][q_cap]
+ *   collected device, fp32 [n_layers][batch][n_kv_heads][capacity] (all layers of the cache), or NULL: nothing yet.  It may be `weight`.
+ *             Not read where decay is 0.
+ *   weight    device, fp32 [n_layers][batch][n_kv_heads][capacity]; rows at or beyond cache_len[b], and other layers, are left as they were
+ *   other arguments as dlm_freecache_attn_step.  A NaN decay is DLM_ERR_UNSUPPORTED.
+ * Supported: head_dim in {64, 128}; n_q_heads a multiple of n_kv_heads; q_cap <= 4096; 16-byte aligned q and cache.
+ * Data-dependent: lengths out of range are clamped and recorded as DLM_ERR_CAPACITY; an expired device wait as DLM_ERR_TIMEOUT.
+ */
+int dlm_cache_weight_accumulate(dlm_ctx* ctx, const dlm_kv_cache* cache, int layer_begin, int layer_end, const void* q,
+                                const float* lse, int n_q_heads, int q_cap, const int32_t* q_len, float softmax_scale,
+                                int cache_len_hint, const float* collected, float decay, float* weight, void* stream);
+int dlm_cache_weight_accumulate_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* cache, int layer_begin, int layer_end, const void* q,
+                                   const float* lse, int n_q_heads, int q_cap, const int32_t* q_len, float softmax_scale,
+                                   int cache_len_hint, const float* collected, float decay, float* weight, void* stream);
+
+/*
+ * dlm_kv_cache_evict, dlm_kv_cache_evict_q4 — brings every sequence down to `keep` cached rows: of each (layer, batch element, KV head)
+ * the rows of largest weight stay.  With len = cache_len[b] and n(b) = min(keep, len), the rows kept are first the protected ones, i < protect_first and
+ * i >= len - protect_last, then those of largest weight, ties to the lowest row; a NaN weight counts as less than any other.
+ * Attention does not depend on the order of the cached rows (keys carry their positions), so kept rows below n(b) stay where they
+ * are and the others move into the places of evicted rows below n(b), the k-th of them (in row order) to the k-th place.  Then
+ * cache_len[b] = n(b); all layers and heads are evicted alike, since they share it.
+ *   weight      device, fp32 [n_layers][batch][n_kv_heads][capacity], as dlm_cache_weight_accumulate leaves it
+ *   keep        1 .. capacity;  protect_first, protect_last >= 0, together at most keep  (else DLM_ERR_SHAPE)
+ *   kept_idx    device, int32 [n_layers][batch][n_kv_heads][keep], out: the row that place i holds now, entries at or beyond n(b) -1
+ *   weight_out  device, fp32 like weight, or NULL: the weight of the row that place i < n(b) holds now; 0 for i in [n(b), len); other entries
+ *               are left as they were.  It may be `weight` itself, but not overlap it otherwise.
+ * The contents of rows at or beyond n(b) are left as they were.  A row that moved is no longer among the last: a caller who wants to protect it again sets its
+ * weight to +infinity.
+ * Data-dependent: cache_len[b] outside [0, capacity]: nothing is evicted for b, its kept_idx are -1, DLM_ERR_CAPACITY.
+ * Supported: bf16 head_dim a multiple of 8, 16-byte aligned k and v; capacity <= 1048576; n_layers * batch * n_kv_heads * ceil(keep / 32) < 2^31 - 256.
+ */
+int dlm_kv_cache_evict(dlm_ctx* ctx, const dlm_kv_cache* cache, const float* weight, int keep, int protect_first,
+                       int protect_last, int32_t* kept_idx, float* weight_out, void* stream);
+int dlm_kv_cache_evict_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* cache, const float* weight, int keep, int protect_first,
+                          int protect_last, int32_t* kept_idx, float* weight_out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -33,6 +33,12 @@ class dlm_kv_cache(ctypes.Structure):
                 ("capacity", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
 
 
+class dlm_kv_cache_q4(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("cache_len", ctypes.c_void_p), ("n_layers", ctypes.c_int32), ("batch", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("capacity", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -47,7 +53,7 @@ def lib() -> ctypes.CDLL:
                           "(there is no CPU or PyTorch fallback)")
     L = ctypes.CDLL(path)
     vp, i32, sz, u64, ip = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_uint64, ctypes.POINTER(ctypes.c_int)
-    cache = ctypes.POINTER(dlm_kv_cache)
+    cache, cache_q4 = ctypes.POINTER(dlm_kv_cache), ctypes.POINTER(dlm_kv_cache_q4)
     for name, restype, argtypes in (
             ("dlm_create", i32, [ctypes.POINTER(vp), i32]),
             ("dlm_destroy", i32, [vp]),
@@ -55,6 +61,7 @@ def lib() -> ctypes.CDLL:
             ("dlm_strerror", ctypes.c_char_p, [i32]),
             ("dlm_launch_count", ctypes.c_int64, [vp]),
             ("dlm_attn_workspace_bytes", sz, [vp, cache, i32, i32, i32]),
+            ("dlm_attn_workspace_bytes_q4", sz, [vp, cache_q4, i32, i32, i32]),
             ("dlm_unmask_workspace_bytes", sz, [vp, i32, i32, i32]),
             ("dlm_unmask_scored_workspace_bytes", sz, [vp, i32, i32, i32]),
             ("dlm_window_proj_workspace_bytes", sz, [vp, i32, i32, i32]),
@@ -122,9 +129,29 @@ def make_kv_cache(k: torch.Tensor, v: torch.Tensor, cache_len: torch.Tensor) -> 
     return c
 
 
+def make_kv_cache_q4(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
+                     cache_len: torch.Tensor) -> dlm_kv_cache_q4:
+    """View of caller-owned tensors: k, v uint8 [NL,B,Hkv,Lcap,D/2]; k_scale, v_scale uint8 [NL,B,Hkv,Lcap,D/32]; cache_len int32 [B]."""
+    if k.dtype != torch.uint8 or k.shape != v.shape or k.dim() != 5:
+        raise TypeError("k and v must be uint8 tensors of the same 5-d shape")
+    NL, B, Hkv, Lcap, half = k.shape
+    if half % 16 != 0 or k_scale.dtype != torch.uint8 or k_scale.shape != (NL, B, Hkv, Lcap, half // 16) or k_scale.shape != v_scale.shape:
+        raise TypeError("k_scale and v_scale must be uint8 tensors with one entry per 32 values of k and v")
+    if cache_len.shape != (B,):
+        raise TypeError("cache_len must have shape [batch]")
+    c = dlm_kv_cache_q4(_ptr(k).value, _ptr(v).value, _ptr(k_scale).value, _ptr(v_scale, torch.uint8).value,
+                        _ptr(cache_len, torch.int32).value, NL, B, Hkv, Lcap, 2 * half)
+    c._keepalive = (k, v, k_scale, v_scale, cache_len)
+    return c
+
+
 def dlm_attn_workspace_bytes(ctx, cache, n_layers_in_call, n_q_heads, q_cap) -> int:
     return int(lib().dlm_attn_workspace_bytes(ctx, ctypes.byref(cache), int(n_layers_in_call), int(n_q_heads),
                                               int(q_cap)))
+
+
+def dlm_attn_workspace_bytes_q4(ctx, cache, n_layers_in_call, n_q_heads, q_cap) -> int:
+    return int(lib().dlm_attn_workspace_bytes_q4(ctx, ctypes.byref(cache), int(n_layers_in_call), int(n_q_heads), int(q_cap)))
 
 
 def dlm_selftest_attn_schedule(ctx, cache, n_layers_in_call, n_q_heads, q_cap, cache_len_hint=0) -> dict:
@@ -180,7 +207,7 @@ def _load_calls():
             raise ImportError(f"{_build.CALLS} cannot be loaded ({e}): run `python -m paper_2505_21467_b200.build` "
                               "(there is no CPU or PyTorch fallback)") from e
         m.set_error(DlmError)
-        m.set_types(ctypes.c_void_p, dlm_kv_cache)
+        m.set_types(ctypes.c_void_p, dlm_kv_cache, dlm_kv_cache_q4)
         _calls = m
     return _calls
 
@@ -198,5 +225,7 @@ except ImportError:
     pass
 for _name in ("dlm_kv_cache_commit", "dlm_freecache_attn_step", "dlm_unmask_select", "dlm_unmask_select_static",
               "dlm_unmask_select_scored", "dlm_guided_accept", "dlm_guided_accept_topk", "dlm_guided_accept_threshold",
-              "dlm_window_qkv_project", "dlm_window_qkv_project_rope", "dlm_window_qkv_project_stage", "dlm_window_out_project"):
+              "dlm_window_qkv_project", "dlm_window_qkv_project_rope", "dlm_window_qkv_project_stage", "dlm_window_out_project",
+              "dlm_kv_cache_commit_q4", "dlm_kv_cache_read_q4", "dlm_freecache_attn_step_q4", "dlm_cache_weight_accumulate",
+              "dlm_cache_weight_accumulate_q4", "dlm_kv_cache_evict", "dlm_kv_cache_evict_q4"):
     globals()[_name] = getattr(_calls, _name) if _calls is not None else _stand_in(_name)

@@ -1,0 +1,692 @@
+// dlm_freecache_attn_step_q4: attention of the active window over [4-bit cache rows ; fresh bf16 rows].
+//
+// The arithmetic is dlm_freecache_attn_step's: scores S = Q K^T in fp32, an online softmax with base-2 exponentials, O += P V with P in
+// bf16 and O in fp32, everything on the tensor cores with S, P and O in TMEM.  A value of the cache has 7 significant bits, so the
+// bf16 tile that the products read holds it exactly; what is quantised is what was committed, nothing on the way.
+//
+// One unit is (layer, batch element, KV head, chunk of up to 256 query rows); its keys are taken in steps of 64, first the cache's,
+// then the fresh ones.  Block = 16 warps:
+//   warps 0-3    softmax of M tile 0 (128 query rows; thread = row = TMEM lane)
+//   warps 4-7    softmax of M tile 1, or with one M tile decoders like 8-11
+//   warps 8-11   decoders: packed K and V steps to bf16 operand tiles, a group of 32 values a thread at a time; one of their lanes
+//                has fresh rows copied straight into operand tiles (TMA)
+//   warp  12     producer (one lane): bulk copies of packed steps (a step's rows lie one after the other), TMA of Q
+//   warps 13, 14 tcgen05.mma issuers of M tile 0 / 1 (one lane each)
+// A step costs the tensor pipe about 1000 cycles with two M tiles, the softmax as much and the decoders 300 of each scheduler's issue
+// slots, so decoding is hidden; with one M tile it costs 500, and twice as many warps decode.
+//
+// Every (unit, step) pair is one item of a global list and block c takes a contiguous share of it, at least `min_share` items: whole
+// units are finished by the block; a share's first and last unit may be a part, whose unnormalised O, maximum and sum go to the
+// workspace.  A second, small launch joins the parts in block order (the result does not depend on timing), so that no block waits for
+// another.
+#include <cuda_bf16.h>
+#include <math_constants.h>
+
+#include "attn_softmax.cuh"
+#include "common.cuh"
+#include "deal.cuh"
+#include "q4_tiles.cuh"
+
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kStep = 64;                 // keys
+constexpr int kMaxBatch = 1024;
+constexpr int kMaxQCap = 4096;
+constexpr int kMaxGrid = 256;
+constexpr int kTmemCols = 512;
+constexpr int kRegsLaunch = 128;          // 512 threads: all of an SM's registers
+constexpr int kRegsSoftmax = 168, kRegsDecode = 104, kRegsControl = 72;
+static_assert(2 * kRegsSoftmax + kRegsDecode + kRegsControl <= 4 * kRegsLaunch, "register split of two M tiles");
+static_assert(kRegsSoftmax + 2 * kRegsDecode + kRegsControl <= 4 * kRegsLaunch, "register split of one M tile");
+constexpr int kBarrierBytes = 512, kFlagBytes = 64;
+
+template <int D, int NMT>
+struct Shape {
+  static constexpr int kPanels = D / 64;
+  static constexpr int kQPanel = 128 * 128;                  // bytes: 128 rows of 64 values
+  static constexpr int kQTile = kPanels * kQPanel;
+  static constexpr int kPanel = kStep * 128;
+  static constexpr int kTile = kPanels * kPanel;             // a step of K or V
+  static constexpr int kPackedStage = 2 * q4::Packed<D>::kBytes;
+  static constexpr int KS = NMT == 2 ? 4 : 3, VS = 3;        // operand tiles
+  static constexpr int PS = NMT == 2 ? 4 : 8;                // packed steps in flight: with one M tile HBM is the bound
+  static constexpr int kDecodeWarps = NMT == 2 ? 4 : 8;
+  static constexpr int kTiles = NMT * kQTile + (KS + VS) * kTile + PS * kPackedStage;
+  static constexpr uint32_t kColO = 0, kColS = 2 * D;        // O[mt] at mt * D, S[mt] at 2 D + mt * 128 (P in its place)
+};
+
+struct Params {
+  const int32_t* cache_len;
+  const int32_t* q_len;
+  const uint8_t *k, *v, *k_scale, *v_scale;
+  __nv_bfloat16* out;
+  float* lse;
+  float4* ws_o;     // [slot][D / 4][rows_pad]: a part's O, four columns of a row a vector
+  float2* ws_ml;    // [slot][rows_pad]: its running maximum (log2 units) and sum
+  int nl, layer_begin, batch, n_kv_heads, n_q_heads, group, capacity, q_cap;
+  int rows_total;   // group * q_cap: query rows of a KV head
+  int n_rc, chunk, rows, rows_pad;   // row chunks, rows of a full chunk (128 or 256), rows of a unit, those in whole warps
+  int fresh_box;    // rows of a TMA box of fresh K / V
+  int min_share;
+  FastDiv by_batch, by_rc, by_kv_heads, by_q_cap;
+  float scale_log2;
+  int* status;
+};
+
+__device__ __forceinline__ int steps_of(int Lc, int Lq) { return Lq <= 0 ? 0 : (Lc + kStep - 1) / kStep + (Lq + kStep - 1) / kStep; }
+
+__device__ __forceinline__ void read_lengths(const Params& p, const Lengths& s, volatile int* any_empty) {
+  read_lengths(p.cache_len, p.q_len, p.batch, p.capacity, p.q_cap, p.status, s, any_empty, steps_of);
+}
+__device__ __forceinline__ Deal deal_of(const Params& p, const Lengths& s, int grid) {
+  return Deal(s.prefix[p.batch], p.nl * p.n_kv_heads * p.n_rc, grid, p.min_share);
+}
+
+struct Segment {
+  int layer, b, kvh, rc;      // layer of the call
+  int Lc, Lq, n_c;            // lengths, steps of the cache
+  int unit_begin;             // item
+  int begin, end;             // steps of the unit
+  int slot;                   // where a part goes, -1: the unit is whole
+};
+
+// The unit that an item belongs to (not its part).
+__device__ __forceinline__ void find_unit(const Params& p, const Lengths& s, const Deal& d, int item, Segment& g) {
+  int rest;
+  const int grp = d.group_of(item, rest);
+  g.b = element_of(s, p.batch, rest);
+  g.layer = p.by_kv_heads.divmod(p.by_rc.divmod(grp, g.rc), g.kvh);
+  g.Lc = s.lc[g.b];
+  g.Lq = s.lq[g.b];
+  g.n_c = (g.Lc + kStep - 1) / kStep;
+  g.unit_begin = grp * d.sum + s.prefix[g.b];
+}
+
+// Walks the segments of a block, alike in every role.
+struct Walk {
+  const Params& p;
+  const Lengths& s;
+  const Deal& d;
+  int at, first, end;
+  __device__ __forceinline__ Walk(const Params& p_, const Lengths& s_, const Deal& d_, int cta) : p(p_), s(s_), d(d_) {
+    at = first = cta < d.n ? d.lo(cta) : 0;
+    end = cta < d.n ? d.lo(cta + 1) : 0;
+  }
+  __device__ __forceinline__ bool next(Segment& g) {
+    if (at >= end) return false;
+    find_unit(p, s, d, at, g);
+    const int steps = s.prefix[g.b + 1] - s.prefix[g.b];
+    g.begin = at - g.unit_begin;
+    g.end = min(steps, end - g.unit_begin);
+    g.slot = g.begin == 0 && g.end == steps ? -1 : at == first ? 2 * (int)blockIdx.x : 2 * (int)blockIdx.x + 1;
+    at = g.unit_begin + g.end;
+    return true;
+  }
+};
+
+__device__ __forceinline__ int step_keys(const Segment& g, int t) {
+  return t < g.n_c ? min(kStep, g.Lc - t * kStep) : min(kStep, g.Lq - (t - g.n_c) * kStep);
+}
+
+template <int D, int NMT, bool kNoWait>
+__global__ void __launch_bounds__(kThreads, 1)
+q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_kn,
+                    const __grid_constant__ CUtensorMap tm_vn, const __grid_constant__ Params p) {
+  using G = Shape<D, NMT>;
+  using Pk = q4::Packed<D>;
+  constexpr uint64_t kLimit = kNoWait ? 0ull : kWaitLimitNs;
+  constexpr int KS = G::KS, VS = G::VS, PS = G::PS;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t smem_pad = (1024u - (smem_u32(smem_raw) & 1023u)) & 1023u;
+  const uint32_t sm_q = smem_u32(smem_raw) + smem_pad;
+  const uint32_t sm_k = sm_q + NMT * G::kQTile, sm_v = sm_k + KS * G::kTile, sm_p = sm_v + VS * G::kTile, sm_bar = sm_p + PS * G::kPackedStage;
+  int* const flags = reinterpret_cast<int*>(smem_raw + smem_pad + G::kTiles + kBarrierBytes);
+  volatile int* const abort_ptr = flags;        // raised by the first wait that gives up
+  volatile int* const never_ptr = flags + 1;    // for waits that must not be cut short by an abort; raised by one that runs out
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(flags + 2);
+  volatile int* const any_empty = flags + 3;
+  const Lengths len(flags + kFlagBytes / 4, p.batch);
+
+  const uint32_t bar_q_full = sm_bar, bar_q_empty = sm_bar + 8, bar_drain = sm_bar + 16;              // drain [2]
+  const uint32_t bar_s_ready = sm_bar + 32, bar_p_ready = sm_bar + 64, bar_pv_done = sm_bar + 96;     // [M tile][buffer]
+  const uint32_t bar_k_full = sm_bar + 128, bar_k_empty = bar_k_full + 8 * KS, bar_v_full = bar_k_empty + 8 * KS, bar_v_empty = bar_v_full + 8 * VS;
+  const uint32_t bar_kf = bar_v_empty + 8 * VS, bar_vf = bar_kf + 8 * KS;                             // fresh rows copied
+  const uint32_t bar_p_full = bar_vf + 8 * VS, bar_p_empty = bar_p_full + 8 * PS;
+  static_assert(128 + 8 * (3 * KS + 3 * VS + 2 * PS) <= kBarrierBytes, "barriers");
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  // warps whose 32 query rows exist, of each M tile
+  auto live_warps = [&](int mt) { return (max(32, min(128, p.rows - 128 * mt)) + 31) / 32; };
+
+  if (tid == 0) {
+    *abort_ptr = 0; *never_ptr = 0; *any_empty = 0;
+    mbar_init(bar_q_full, 1);
+    mbar_init(bar_q_empty, NMT);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar_drain + 8 * i, 1);
+      for (int u = 0; u < 2; ++u) {
+        mbar_init(bar_s_ready + 16 * i + 8 * u, 1);
+        mbar_init(bar_p_ready + 16 * i + 8 * u, (uint32_t)live_warps(i));
+        mbar_init(bar_pv_done + 16 * i + 8 * u, 1);
+      }
+    }
+    for (int i = 0; i < KS; ++i) {
+      mbar_init(bar_k_full + 8 * i, G::kDecodeWarps);
+      mbar_init(bar_k_empty + 8 * i, NMT);
+      mbar_init(bar_kf + 8 * i, 1);
+    }
+    for (int i = 0; i < VS; ++i) {
+      mbar_init(bar_v_full + 8 * i, G::kDecodeWarps);
+      mbar_init(bar_v_empty + 8 * i, NMT);
+      mbar_init(bar_vf + 8 * i, 1);
+    }
+    for (int i = 0; i < PS; ++i) {
+      mbar_init(bar_p_full + 8 * i, 1);
+      mbar_init(bar_p_empty + 8 * i, G::kDecodeWarps);
+    }
+    mbar_fence_init();
+    fence_proxy_async_smem();
+  }
+  if (warp == 13) {
+    tmem_alloc(smem_u32(tmem_slot), kTmemCols);
+    tmem_relinquish();
+  }
+  if (warp == 12 && lane == 0) {
+    prefetch_tensormap(&tm_q);
+    prefetch_tensormap(&tm_kn);
+    prefetch_tensormap(&tm_vn);
+  }
+  dlm_grid_dependency_wait();
+  dlm_trigger_dependents();
+  if (warp == 0) read_lengths(p, len, any_empty);
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = *tmem_slot;
+  const Deal deal = deal_of(p, len, (int)gridDim.x);
+
+  if (warp >= 12) {
+    setmaxnreg_dec<kRegsControl>();
+    if (warp == 12 && lane == 0) {
+      // ================================================================= producer
+      Walk walk(p, len, deal, blockIdx.x);
+      Segment g = {};
+      uint32_t ps = 0, n_q = 0;   // packed steps and Q tiles so far
+      bool ok = true, q_due = false;
+      auto issue_q = [&]() {
+        q_due = false;
+        if (n_q > 0 && !mbar_wait_limit(bar_q_empty, (n_q - 1) & 1, abort_ptr, kLimit)) return false;
+        const int z = (g.layer * p.batch + g.b) * p.n_kv_heads + g.kvh;
+        mbar_expect_tx(bar_q_full, (uint32_t)(NMT * min(128, p.rows)) * 128u * G::kPanels);   // a box counts in full
+        for (int mt = 0; mt < NMT; ++mt)
+          for (int pn = 0; pn < G::kPanels; ++pn)
+            tma_load_3d(sm_q + mt * G::kQTile + pn * G::kQPanel, &tm_q, bar_q_full, pn * 64, g.rc * p.chunk + mt * 128, z);
+        ++n_q;
+        return true;
+      };
+      // Q is copied as soon as the unit before has done with its own, and at the latest where this lane would wait for the
+      // steps that need it
+      auto wait = [&](uint32_t bar, uint32_t parity) {
+        if (q_due && ((n_q == 0 || mbar_test_wait(bar_q_empty, (n_q - 1) & 1)) || !mbar_test_wait(bar, parity)) && !issue_q()) return false;
+        return mbar_wait_limit(bar, parity, abort_ptr, kLimit);
+      };
+      while (ok && walk.next(g)) {
+        q_due = true;
+        if (n_q == 0) ok = issue_q();
+        const size_t head = ((size_t)(g.layer + p.layer_begin) * p.batch + g.b) * p.n_kv_heads + g.kvh;
+        for (int t = g.begin; t < min(g.end, g.n_c) && ok; ++t, ++ps) {
+          const uint32_t s = ps % PS, dst = sm_p + s * G::kPackedStage, bar = bar_p_full + 8 * s;
+          if (ps >= (uint32_t)PS) ok = wait(bar_p_empty + 8 * s, (ps / PS - 1) & 1);
+          if (!ok) break;
+          const int rows = step_keys(g, t);
+          const size_t row = head * p.capacity + (size_t)t * kStep;
+          mbar_expect_tx(bar, 2 * Pk::bytes(rows));
+          Pk::copy(dst, p.k, p.k_scale, row, rows, bar);
+          Pk::copy(dst + Pk::kBytes, p.v, p.v_scale, row, rows, bar);
+        }
+        if (ok && q_due) ok = issue_q();
+      }
+      // no copy lands after the block has released its shared memory
+      for (uint32_t i = ps > (uint32_t)PS ? ps - PS : 0; i < ps; ++i) mbar_wait(bar_p_full + 8 * (i % PS), (i / PS) & 1, never_ptr);
+      if (n_q > 0) mbar_wait(bar_q_full, (n_q - 1) & 1, never_ptr);
+    } else if ((warp == 13 || warp == 14) && warp - 13 < NMT && elect_one_sync()) {
+      // ================================================================= MMA issuers, one lane each
+      const int mt = warp - 13;
+      auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_limit(bar, parity, abort_ptr, kLimit); };
+      Walk walk(p, len, deal, blockIdx.x);
+      Segment g = {};
+      uint32_t st = 0, pt = 0, seg = 0;   // steps whose scores / whose P V product have been issued
+      bool ok = true;
+      const uint32_t idesc_pv = make_idesc_bf16(128, D, 1);
+      const uint64_t desc_q = make_smem_desc_sw128(sm_q + mt * G::kQTile, 16, 1024);
+      const uint64_t desc_k0 = make_smem_desc_sw128(sm_k, 16, 1024);
+      const uint64_t desc_v0 = make_smem_desc_sw128(sm_v, G::kPanel, 1024);
+      const uint32_t t_o = tmem + G::kColO + mt * D, t_s = tmem + G::kColS + mt * 128;
+      while (ok && walk.next(g)) {
+        ok = wait(bar_q_full, seg & 1);
+        if (!ok) break;
+        int ts = g.begin;
+        // scores of the next step that has none yet, into buffer st & 1
+        auto issue_s = [&]() -> bool {
+          if (ts >= g.end) return true;
+          const uint32_t ks = st % KS;
+          if (!wait(bar_k_full + 8 * ks, (st / KS) & 1)) return false;
+          tc_fence_after_sync();
+          const uint32_t idesc = make_idesc_bf16(128, (uint32_t)((step_keys(g, ts) + 15) & ~15), 0);
+          const uint64_t dk = desc_offset(desc_k0, ks * G::kTile);
+          const uint32_t d = t_s + (st & 1) * kStep;
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            const uint32_t a = ((k >> 2) * G::kQPanel + (k & 3) * 32) >> 4, b = ((k >> 2) * G::kPanel + (k & 3) * 32) >> 4;
+            mma_ss_lo<false>(d, (uint32_t)desc_q + a, (uint32_t)dk + b, (uint32_t)(desc_q >> 32), idesc, k > 0 ? 1u : 0u);
+          }
+          tc_commit(bar_s_ready + 16 * mt + 8 * (st & 1));
+          tc_commit(bar_k_empty + 8 * ks);
+          ++st;
+          if (++ts >= g.end) tc_commit(bar_q_empty);   // Q is not read again in this segment
+          return true;
+        };
+        ok = issue_s() && issue_s();
+        for (int t = g.begin; t < g.end && ok; ++t, ++pt) {
+          const uint32_t vs = pt % VS, buf = pt & 1;
+          ok = wait(bar_v_full + 8 * vs, (pt / VS) & 1) && wait(bar_p_ready + 16 * mt + 8 * buf, (pt >> 1) & 1);
+          if (!ok) break;
+          tc_fence_after_sync();
+          const int n16 = (step_keys(g, t) + 15) & ~15;
+          const uint64_t dv = desc_offset(desc_v0, vs * G::kTile);
+          const uint32_t a = t_s + buf * kStep;
+          if (t == g.begin) mma_ts<false>(t_o, a, dv, idesc_pv); else mma_ts<true>(t_o, a, dv, idesc_pv);
+          if (n16 == kStep) {
+#pragma unroll
+            for (int i = 1; i < kStep / 16; ++i) mma_ts<true>(t_o, a + i * 8, desc_offset(dv, i * 2048), idesc_pv);
+          } else {
+            for (int i = 1; i < n16 / 16; ++i) mma_ts<true>(t_o, a + i * 8, desc_offset(dv, i * 2048), idesc_pv);
+          }
+          tc_commit(bar_pv_done + 16 * mt + 8 * buf);
+          tc_commit(bar_v_empty + 8 * vs);
+          ok = issue_s();   // the buffer just consumed takes the step after next
+        }
+        ++seg;
+      }
+      // every MMA issued by this lane has finished before TMEM and shared memory are released
+      tc_commit(bar_drain + 8 * mt);
+      mbar_wait(bar_drain + 8 * mt, 0, never_ptr);
+    }
+  } else if (warp >= 8 || (NMT == 1 && warp >= 4)) {
+    // ================================================================= decoders
+    setmaxnreg_dec<kRegsDecode>();
+    constexpr int kDecoders = G::kDecodeWarps * 32, kTasks = kStep * (D / q4::kGroup), kPer = (kTasks + kDecoders - 1) / kDecoders;
+    const int me = tid - (kThreads - 128 - kDecoders);
+    auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_warp(bar, parity, abort_ptr, kLimit); };
+    // what was stored to a tile is visible to the tensor cores before the tile is announced
+    auto announce = [&](uint32_t bar) {
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar);
+    };
+    Walk walk(p, len, deal, blockIdx.x);
+    Segment g = {};
+    uint32_t st = 0, ps = 0, fs = 0, fk = 0, fv = 0;   // steps, packed and fresh ones so far; fresh K and V tiles asked for (by one lane)
+    bool ok = true;
+    while (ok && walk.next(g)) {
+      int t_k = max(g.n_c, g.begin), t_v = t_k;   // the fresh steps whose K and V are asked for next
+      for (int t = g.begin; t < g.end && ok; ++t, ++st) {
+        // One lane of the decoders copies the fresh rows, as far ahead as there are operand tiles free.  (Not the producer: it runs further
+        // ahead of the products than a stage's barrier can tell, since a wait for a phase works only when the one before it is over.)
+        if (me == 0 && ((t_k < g.end && t_k - t < KS) || (t_v < g.end && t_v - t < VS))) {
+          const int z = (g.layer * p.batch + g.b) * p.n_kv_heads + g.kvh;
+          const uint32_t bytes = (uint32_t)p.fresh_box * 128u * G::kPanels;
+          // the stage is free: for the step at hand wait for that, for later ones only look
+          auto free_stage = [&](uint32_t bar, uint32_t use, bool now) {
+            if (use == 0) return true;
+            return now ? mbar_wait_limit(bar, (use - 1) & 1, abort_ptr, kLimit) : mbar_test_wait(bar, (use - 1) & 1);
+          };
+          for (; t_k < g.end && t_k - t < KS; ++t_k, ++fk) {
+            const uint32_t i = st + (t_k - t), s = i % KS, bar = bar_kf + 8 * (fk % KS);
+            if (!free_stage(bar_k_empty + 8 * s, i / KS, t_k == t)) break;
+            mbar_expect_tx(bar, bytes);
+            for (int pn = 0; pn < G::kPanels; ++pn) tma_load_3d(sm_k + s * G::kTile + pn * G::kPanel, &tm_kn, bar, pn * 64, (t_k - g.n_c) * kStep, z);
+          }
+          for (; t_v < g.end && t_v - t < VS; ++t_v, ++fv) {
+            const uint32_t i = st + (t_v - t), s = i % VS, bar = bar_vf + 8 * (fv % VS);
+            if (!free_stage(bar_v_empty + 8 * s, i / VS, t_v == t)) break;
+            mbar_expect_tx(bar, bytes);
+            for (int pn = 0; pn < G::kPanels; ++pn) tma_load_3d(sm_v + s * G::kTile + pn * G::kPanel, &tm_vn, bar, pn * 64, (t_v - g.n_c) * kStep, z);
+          }
+        }
+        __syncwarp();
+        const uint32_t ks = st % KS, vs = st % VS;
+        const uint32_t k_tile = sm_k + ks * G::kTile, v_tile = sm_v + vs * G::kTile;
+        const int keys = step_keys(g, t), n16 = (keys + 15) & ~15;
+        if (t < g.n_c) {
+          const uint32_t s = ps % PS, packed = sm_p + s * G::kPackedStage;
+          ok = wait(bar_p_full + 8 * s, (ps / PS) & 1);
+          if (!ok) break;
+          q4::Group32 kg[kPer], vg[kPer];
+          const int tasks = keys * (D / q4::kGroup);
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) {
+            const int task = me + i * kDecoders;
+            if (task < tasks) {
+              kg[i] = q4::read_group<D>(packed, task);
+              vg[i] = q4::read_group<D>(packed + Pk::kBytes, task);
+            }
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar_p_empty + 8 * s);
+          ++ps;
+          if (st >= (uint32_t)KS) ok = wait(bar_k_empty + 8 * ks, (st / KS - 1) & 1);
+          if (!ok) break;
+#pragma unroll
+          for (int i = 0; i < kPer; ++i)
+            if (me + i * kDecoders < tasks) q4::write_group<D>(k_tile, G::kPanel, me + i * kDecoders, kg[i]);
+          announce(bar_k_full + 8 * ks);
+          if (st >= (uint32_t)VS) ok = wait(bar_v_empty + 8 * vs, (st / VS - 1) & 1);
+          if (!ok) break;
+#pragma unroll
+          for (int i = 0; i < kPer; ++i)
+            if (me + i * kDecoders < tasks) q4::write_group<D>(v_tile, G::kPanel, me + i * kDecoders, vg[i]);
+        } else {
+          ok = wait(bar_kf + 8 * (fs % KS), (fs / KS) & 1);
+          if (!ok) break;
+          announce(bar_k_full + 8 * ks);
+          ok = wait(bar_vf + 8 * (fs % VS), (fs / VS) & 1);
+          if (!ok) break;
+          ++fs;
+        }
+        // V rows from `keys` to the next multiple of 16 meet P = 0: clear them, so that a NaN left there cannot reach O
+        for (int i = keys * (D / 8) + me; i < n16 * (D / 8); i += kDecoders) q4::clear_piece<D>(v_tile, G::kPanel, i);
+        announce(bar_v_full + 8 * vs);
+      }
+    }
+    // no copy lands after the block has released its shared memory (here and in the producer: they have landed long since unless the
+    // block is unwinding)
+    for (uint32_t i = fk > (uint32_t)KS ? fk - KS : 0; i < fk; ++i) mbar_wait(bar_kf + 8 * (i % KS), (i / KS) & 1, never_ptr);
+    for (uint32_t i = fv > (uint32_t)VS ? fv - VS : 0; i < fv; ++i) mbar_wait(bar_vf + 8 * (i % VS), (i / VS) & 1, never_ptr);
+  } else {
+    // ================================================================= softmax warps (those that own real rows)
+    setmaxnreg_inc<kRegsSoftmax>();
+    const int mt = warp >> 2, row = (warp & 3) * 32 + lane, r_unit = mt * 128 + row;
+    if ((warp & 3) < live_warps(mt)) {
+      const uint32_t t_lane = (uint32_t)((warp & 3) * 32) << 16;
+      const uint32_t t_s = tmem + t_lane + G::kColS + mt * 128, t_o = tmem + t_lane + G::kColO + mt * D;
+      auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_warp(bar, parity, abort_ptr, kLimit); };
+      auto out_row = [&](int layer, int b, int kvh, int rc) {
+        return (((size_t)layer * p.batch + b) * p.n_q_heads + (size_t)kvh * p.group) * p.q_cap + rc * p.chunk + r_unit;
+      };
+      if (*any_empty) {
+        // units without any key (inactive batch elements) appear in no share: their rows are zero
+        const int n_units = p.nl * p.n_kv_heads * p.n_rc * p.batch;
+        for (int unit = blockIdx.x; unit < n_units; unit += gridDim.x) {
+          int b, rc, kvh;
+          const int layer = p.by_kv_heads.divmod(p.by_rc.divmod(p.by_batch.divmod(unit, b), rc), kvh);
+          if (len.prefix[b + 1] != len.prefix[b] || r_unit >= p.rows || rc * p.chunk + r_unit >= p.rows_total) continue;
+          const size_t r = out_row(layer, b, kvh, rc);
+#pragma unroll
+          for (int c = 0; c < D / 8; ++c) reinterpret_cast<uint4*>(p.out + r * D)[c] = make_uint4(0, 0, 0, 0);
+          if (p.lse) p.lse[r] = -CUDART_INF_F;
+        }
+      }
+      Walk walk(p, len, deal, blockIdx.x);
+      Segment g = {};
+      uint32_t st = 0;
+      bool ok = true;
+      while (ok && walk.next(g)) {
+        float m_used = -CUDART_INF_F, l_run = 0.f;
+        for (int t = g.begin; t < g.end; ++t, ++st) {
+          const uint32_t buf = st & 1, before = 16 * mt + 8 * ((st - 1) & 1), parity = ((st - 1) >> 1) & 1;
+          ok = wait(bar_s_ready + 16 * mt + 8 * buf, (st >> 1) & 1);
+          if (!ok) break;
+          tc_fence_after_sync();
+          const int keys = step_keys(g, t);
+          if (keys == kStep)
+            ok = softmax_half_full<D>(t_s + buf * kStep, t_o, t == g.begin, p.scale_log2, m_used, l_run, bar_pv_done + before, parity, abort_ptr);
+          else
+            ok = softmax_half_ragged<D>(t_s + buf * kStep, t_o, keys, t == g.begin, p.scale_log2, m_used, l_run, bar_pv_done + before, parity, abort_ptr);
+          if (!ok) break;
+          __syncwarp();
+          if (lane == 0) {
+            tc_fence_before_sync();
+            mbar_arrive(bar_p_ready + 16 * mt + 8 * buf);
+          }
+        }
+        // ---- O is complete once the last P V product has finished
+        if (ok) ok = wait(bar_pv_done + 16 * mt + 8 * ((st - 1) & 1), ((st - 1) >> 1) & 1);
+        if (!ok) break;
+        tc_fence_after_sync();
+        const int r_kv = g.rc * p.chunk + r_unit;
+        const bool real = r_unit < p.rows && r_kv < p.rows_total;
+        uint32_t v[32];
+        if (g.slot < 0) {
+          const bool active = real && r_kv - p.by_q_cap.div(r_kv) * p.q_cap < g.Lq;
+          const float inv = active ? 1.f / l_run : 0.f;
+          const size_t r = out_row(g.layer, g.b, g.kvh, g.rc);
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            tmem_ld32(t_o + c * 32, v);
+            tmem_ld_wait();
+            if (!real) continue;
+            uint4* o = reinterpret_cast<uint4*>(p.out + r * D + c * 32);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t h[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                h[j] = active ? pack_bf16(__uint_as_float(v[i * 8 + 2 * j]) * inv, __uint_as_float(v[i * 8 + 2 * j + 1]) * inv) : 0u;
+              o[i] = make_uint4(h[0], h[1], h[2], h[3]);
+            }
+          }
+          if (real && p.lse) p.lse[r] = active ? (m_used + lg2_approx(l_run)) * 0.6931471805599453f : -CUDART_INF_F;
+        } else {
+          float4* po = p.ws_o + (size_t)g.slot * (D / 4) * p.rows_pad + r_unit;
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            tmem_ld32(t_o + c * 32, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              __stcg(po + (size_t)(c * 8 + j) * p.rows_pad, make_float4(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1]),
+                                                                        __uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3])));
+          }
+          __stcg(p.ws_ml + (size_t)g.slot * p.rows_pad + r_unit, make_float2(m_used, l_run));
+        }
+        tc_fence_before_sync();   // O has been read: the next segment's first product overwrites it once this thread's P is announced
+      }
+    }
+  }
+  // ---- teardown: nothing of this block is in flight any more
+  __syncwarp();
+  tc_fence_before_sync();
+  __syncthreads();
+  if (tid == 0 && (*abort_ptr || *never_ptr)) dlm_set_status(p.status, DLM_ERR_TIMEOUT);
+  if (warp == 13) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, kTmemCols);
+    __syncwarp();
+  }
+}
+
+// Joins the parts of split units.  Every boundary between two shares that lies inside a unit belongs to that unit; the first of them does
+// the work for all its parts.  Block = (boundary, 32 rows); a warp has 8 columns, a lane a row.
+template <int D>
+__global__ void __launch_bounds__(D * 4) q4_attention_join_kernel(const __grid_constant__ Params p, int grid) {
+  extern __shared__ int join_smem[];
+  const Lengths len(join_smem, p.batch);
+  dlm_grid_dependency_wait();
+  dlm_trigger_dependents();
+  if (threadIdx.x < 32) read_lengths(p, len, nullptr);
+  __syncthreads();
+  const Deal d = deal_of(p, len, grid);
+  const int c = blockIdx.x + 1;
+  if (c >= d.n) return;
+  const int boundary = d.lo(c);
+  Segment g;
+  find_unit(p, len, d, boundary, g);
+  if (g.unit_begin == boundary || d.lo(c - 1) > g.unit_begin) return;   // between two units; not the unit's first
+  const int unit_end = g.unit_begin + len.prefix[g.b + 1] - len.prefix[g.b];
+  const int c_first = c - 1, c_last = d.owner(unit_end - 1);
+  const int row = blockIdx.y * 32 + (threadIdx.x & 31), c8 = threadIdx.x >> 5;
+  const int r_kv = g.rc * p.chunk + row;
+  if (row >= p.rows || r_kv >= p.rows_total) return;
+  const bool active = r_kv - p.by_q_cap.div(r_kv) * p.q_cap < g.Lq;
+  const size_t out = (((size_t)g.layer * p.batch + g.b) * p.n_q_heads + (size_t)g.kvh * p.group) * p.q_cap + r_kv;
+  // the part of block b: its first segment if the part starts where its share does, else its second
+  auto slot = [&](int b) { return (size_t)(d.lo(b) >= g.unit_begin ? 2 * b : 2 * b + 1); };
+  float m = -CUDART_INF_F, l = 0.f, o[8] = {};
+  for (int b0 = c_first; b0 <= c_last; b0 += 4) {
+    float2 ml[4];
+    float4 x[4], y[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      ml[j] = make_float2(-CUDART_INF_F, 0.f);
+      x[j] = y[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (b0 + j <= c_last) {
+        const size_t s = slot(b0 + j);
+        const float4* po = p.ws_o + (s * (D / 4) + 2 * c8) * p.rows_pad + row;
+        ml[j] = __ldcg(p.ws_ml + s * p.rows_pad + row);
+        x[j] = __ldcg(po);
+        y[j] = __ldcg(po + p.rows_pad);
+      }
+    }
+    const float m_new = fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), m);
+    const float old = ex2_approx(m - m_new);   // the first time 2^-inf = 0
+    l *= old;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] *= old;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float w = ex2_approx(ml[j].x - m_new);
+      l = fmaf(w, ml[j].y, l);
+      o[0] = fmaf(w, x[j].x, o[0]); o[1] = fmaf(w, x[j].y, o[1]); o[2] = fmaf(w, x[j].z, o[2]); o[3] = fmaf(w, x[j].w, o[3]);
+      o[4] = fmaf(w, y[j].x, o[4]); o[5] = fmaf(w, y[j].y, o[5]); o[6] = fmaf(w, y[j].z, o[6]); o[7] = fmaf(w, y[j].w, o[7]);
+    }
+    m = m_new;
+  }
+  const float inv = 1.f / l;
+  uint32_t h[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) h[j] = active ? pack_bf16(o[2 * j] * inv, o[2 * j + 1] * inv) : 0u;
+  *reinterpret_cast<uint4*>(p.out + out * D + c8 * 8) = make_uint4(h[0], h[1], h[2], h[3]);
+  if (c8 == 0 && p.lse) p.lse[out] = active ? (m + lg2_approx(l)) * 0.6931471805599453f : -CUDART_INF_F;
+}
+
+using Kernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const Params);
+Kernel kernel_of(int D, int n_mt, bool no_wait) {
+  if (D == 128) {
+    if (n_mt == 2) return no_wait ? q4_attention_kernel<128, 2, true> : q4_attention_kernel<128, 2, false>;
+    return no_wait ? q4_attention_kernel<128, 1, true> : q4_attention_kernel<128, 1, false>;
+  }
+  if (n_mt == 2) return no_wait ? q4_attention_kernel<64, 2, true> : q4_attention_kernel<64, 2, false>;
+  return no_wait ? q4_attention_kernel<64, 1, true> : q4_attention_kernel<64, 1, false>;
+}
+
+int shared_bytes(int D, int n_mt, int batch) {
+  const int tiles = D == 128 ? (n_mt == 2 ? Shape<128, 2>::kTiles : Shape<128, 1>::kTiles) : (n_mt == 2 ? Shape<64, 2>::kTiles : Shape<64, 1>::kTiles);
+  return 1024 + tiles + kBarrierBytes + kFlagBytes + 4 * length_ints(batch);
+}
+
+struct Workspace {
+  size_t o_bytes, ml_bytes;
+};
+int rows_of(int n_q_heads, int n_kv_heads, int q_cap) { return n_q_heads / n_kv_heads * q_cap; }
+Workspace workspace_of(const dlm_ctx* ctx, int head_dim, int rows_total) {
+  const size_t slots = 2 * (size_t)(ctx->num_sms < kMaxGrid ? ctx->num_sms : kMaxGrid), pad = (size_t)((rows_total < 256 ? rows_total : 256) + 31) / 32 * 32;
+  return {slots * pad * head_dim * sizeof(float), slots * pad * 2 * sizeof(float)};
+}
+
+}  // namespace
+
+extern "C" size_t dlm_attn_workspace_bytes_q4(const dlm_ctx* ctx, const dlm_kv_cache_q4* cache, int n_layers_in_call,
+                                              int n_q_heads, int q_cap) {
+  if (!ctx || !cache || n_layers_in_call <= 0 || n_q_heads <= 0 || q_cap <= 0 || cache->n_kv_heads <= 0 || cache->batch <= 0 ||
+      (cache->head_dim != 64 && cache->head_dim != 128) || n_q_heads % cache->n_kv_heads != 0 || q_cap > kMaxQCap)
+    return 0;
+  const Workspace w = workspace_of(ctx, cache->head_dim, rows_of(n_q_heads, cache->n_kv_heads, q_cap));
+  return w.o_bytes + w.ml_bytes;
+}
+
+extern "C" int dlm_freecache_attn_step_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* cache, int layer_begin, int layer_end, const void* q,
+                                          const void* k_new, const void* v_new, int n_q_heads, int q_cap, const int32_t* q_len,
+                                          float softmax_scale, int cache_len_hint, void* out, float* lse, void* workspace,
+                                          size_t workspace_bytes, void* stream) {
+  (void)cache_len_hint;
+  if (!ctx || !q || !k_new || !v_new || !out) return DLM_ERR_NULL;
+  const int bad = dlm_check_q4(cache);
+  if (bad != DLM_OK) return bad;
+  if (n_q_heads <= 0 || q_cap <= 0 || layer_begin < 0 || layer_end > cache->n_layers || layer_begin >= layer_end) return DLM_ERR_SHAPE;
+  if (n_q_heads % cache->n_kv_heads != 0) return DLM_ERR_UNSUPPORTED;
+  const int D = cache->head_dim, group = n_q_heads / cache->n_kv_heads, nl = layer_end - layer_begin;
+  if (q_cap > kMaxQCap || (long long)group * q_cap > (1 << 20) || cache->batch > kMaxBatch) return DLM_ERR_UNSUPPORTED;
+  if (((uintptr_t)q | (uintptr_t)k_new | (uintptr_t)v_new | (uintptr_t)out) & 15) return DLM_ERR_UNSUPPORTED;
+  const int rows_total = group * q_cap, n_mt = rows_total > 128 ? 2 : 1, chunk = 128 * n_mt, n_rc = (rows_total + chunk - 1) / chunk;
+  const long long units = (long long)nl * cache->batch * cache->n_kv_heads * n_rc;
+  const long long steps = (cache->capacity + kStep - 1) / kStep + (q_cap + kStep - 1) / kStep;
+  if (units * steps >= (1LL << 30)) return DLM_ERR_UNSUPPORTED;   // items are counted in 32 bits
+  DLM_DEVICE_TRY(ctx);
+  const Workspace ws = workspace_of(ctx, D, rows_total);
+  if (!workspace || workspace_bytes < ws.o_bytes + ws.ml_bytes || ((uintptr_t)workspace & 255)) return DLM_ERR_WORKSPACE;
+  const bool no_wait = ctx->wait_limit_ns == 0;
+  const Kernel kern = kernel_of(D, n_mt, no_wait);
+  const int which = (D == 128 ? 0 : 1) + (n_mt == 2 ? 0 : 2) + (no_wait ? 4 : 0);
+  if (ctx->q4_smem_limit[which] == 0) {
+    cudaFuncAttributes a;
+    DLM_CUDA_TRY(cudaFuncGetAttributes(&a, reinterpret_cast<const void*>(kern)));
+    if (a.numRegs != kRegsLaunch) return DLM_ERR_UNSUPPORTED;   // the register split would wait for ever
+    const int limit = ctx->max_smem_optin - (int)a.sharedSizeBytes;
+    DLM_CUDA_TRY(cudaFuncSetAttribute(reinterpret_cast<const void*>(kern), cudaFuncAttributeMaxDynamicSharedMemorySize, limit));
+    ctx->q4_smem_limit[which] = limit;
+  }
+  const int smem = shared_bytes(D, n_mt, cache->batch);
+  if (smem > ctx->q4_smem_limit[which]) return DLM_ERR_UNSUPPORTED;
+  Params p;
+  p.n_rc = n_rc;
+  p.cache_len = cache->cache_len;
+  p.q_len = q_len;
+  p.k = static_cast<const uint8_t*>(cache->k);
+  p.v = static_cast<const uint8_t*>(cache->v);
+  p.k_scale = static_cast<const uint8_t*>(cache->k_scale);
+  p.v_scale = static_cast<const uint8_t*>(cache->v_scale);
+  p.out = static_cast<__nv_bfloat16*>(out);
+  p.lse = lse;
+  p.ws_o = static_cast<float4*>(workspace);
+  p.ws_ml = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + ws.o_bytes);
+  p.nl = nl;
+  p.layer_begin = layer_begin;
+  p.batch = cache->batch;
+  p.n_kv_heads = cache->n_kv_heads;
+  p.n_q_heads = n_q_heads;
+  p.group = group;
+  p.capacity = cache->capacity;
+  p.q_cap = q_cap;
+  p.rows_total = rows_total;
+  p.chunk = chunk;
+  p.rows = rows_total < chunk ? rows_total : chunk;
+  p.rows_pad = (p.rows + 31) & ~31;
+  p.fresh_box = q_cap < kStep ? q_cap : kStep;
+  p.min_share = 2;
+  p.by_batch = make_fast_div(p.batch);
+  p.by_rc = make_fast_div(p.n_rc);
+  p.by_kv_heads = make_fast_div(p.n_kv_heads);
+  p.by_q_cap = make_fast_div(q_cap);
+  p.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;
+  p.status = &ctx->words->status;
+  CUtensorMap tm_q, tm_kn, tm_vn;
+  const long long slabs = (long long)nl * cache->batch * cache->n_kv_heads;
+  int rc = encode_rows_map(ctx, &tm_q, q, D, rows_total, slabs, p.rows < 128 ? p.rows : 128);
+  if (rc == DLM_OK) rc = encode_rows_map(ctx, &tm_kn, k_new, D, q_cap, slabs, p.fresh_box);
+  if (rc == DLM_OK) rc = encode_rows_map(ctx, &tm_vn, v_new, D, q_cap, slabs, p.fresh_box);
+  if (rc != DLM_OK) return rc;
+  const long long most = units * steps;
+  const int sms = ctx->num_sms < kMaxGrid ? ctx->num_sms : kMaxGrid, grid = most < sms ? (int)most : sms;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  DLM_CUDA_TRY(dlm_launch(kern, dim3(grid), dim3(kThreads), (size_t)smem, st, tm_q, tm_kn, tm_vn, p));
+  if (grid == 1) return dlm_launch_ok(ctx, 1);
+  const dim3 join((unsigned)(grid - 1), (unsigned)(p.rows_pad / 32));
+  const size_t join_smem = 4 * (size_t)length_ints(cache->batch);
+  if (D == 128)
+    DLM_CUDA_TRY(dlm_launch(q4_attention_join_kernel<128>, join, dim3(512), join_smem, st, p, grid));
+  else
+    DLM_CUDA_TRY(dlm_launch(q4_attention_join_kernel<64>, join, dim3(256), join_smem, st, p, grid));
+  return dlm_launch_ok(ctx, 2);
+}

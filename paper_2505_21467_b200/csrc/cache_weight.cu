@@ -1,0 +1,516 @@
+// dlm_cache_weight_accumulate, dlm_cache_weight_accumulate_q4: the attention weight that each cached row gets from the query rows of its KV
+// head, added to what it has collected.
+//
+// With the row's log sum known from the attention step, a weight is exp2(scale log2(e) <q, k> - lse log2(e)): no maximum, no second pass.
+// The product is taken as S^T = K Q^T, keys as the rows of the tensor cores' tile: then a key is a TMEM lane, so a thread, and
+// its sum over the query rows runs along the columns of that lane, in registers and in a fixed order, with no exchange between threads and
+// no atomics.  Per (key, query) the tensor pipe needs 2 D flops and the thread one fused multiply-add, an exponential and an addition.
+//
+// A step is a tile of 128 keys of a (layer, batch element, KV head) against 128 query rows; a tile meets all query rows of its KV head.
+// Block = 16 warps, one block per SM with a contiguous share of the tiles:
+//   warps 0-3, 4-7   sums of every other tile (two score buffers of 128 columns each)
+//   warps 8-11       4-bit cache: decoders of K tiles
+//   warp  12         producer (one lane): K tiles by TMA (bf16) or bulk copies (4 bits), query rows by TMA
+//   warps 13, 14     tcgen05.mma issuers for warps 0-3 / 4-7 (one lane each)
+//   warp  15         the query rows' logarithms, and zeros for query rows that take no part
+// Query rows lie in two slots of 128: up to 256 stay there for all tiles of a unit, more go through for every pair of tiles.
+#include <cuda_bf16.h>
+#include <math_constants.h>
+
+#include "common.cuh"
+#include "deal.cuh"
+#include "q4_tiles.cuh"
+#include "sm100_ptx.cuh"
+
+namespace {
+
+using namespace sm100;
+
+constexpr int kThreads = 512;
+constexpr int kKeys = 128;                // a tile
+constexpr int kRows = 128;                // query rows of a step
+constexpr int kMaxBatch = 1024;
+constexpr int kMaxQCap = 4096;
+constexpr int kMaxGrid = 256;
+constexpr int kTmemCols = 512;
+constexpr int kBarrierBytes = 512, kFlagBytes = 64;
+constexpr int kDecodeWarps = 4;
+
+template <int D>
+struct Shape {
+  static constexpr int kPanels = D / 64;
+  static constexpr int kPanel = 128 * 128;           // bytes: 128 rows of 64 values, K tile and query slot alike
+  static constexpr int kTile = kPanels * kPanel;
+  static constexpr int KS = 4;                       // K tiles, two for either group of warps
+  static constexpr int PS = 3;                       // packed K tiles
+  static constexpr int kPackedStage = 2 * q4::Packed<D>::kBytes;   // two runs of 64 rows
+  static constexpr int kLogBytes = 2 * kRows * 4;
+  static constexpr int kTiles = (2 + KS) * kTile;
+};
+
+struct Params {
+  const int32_t* cache_len;
+  const int32_t* q_len;
+  const uint8_t *k, *k_scale;   // 4-bit cache
+  const float* lse;
+  const float* collected;       // may be `weight`
+  float* weight;
+  float decay;
+  int nl, layer_begin, batch, n_kv_heads, n_q_heads, group, capacity, q_cap;
+  int rows_total, n_qc;         // query rows of a KV head, chunks of 128 of them
+  int q_box, k_box;             // rows of the TMA boxes
+  FastDiv by_kv_heads, by_q_cap;
+  float scale_log2;
+  int* status;
+};
+
+struct Segment {
+  int layer, b, kvh, Lc, Lq;
+  int begin, end;   // tiles of the unit
+};
+
+struct Walk {
+  const Params& p;
+  const Lengths& s;
+  const Deal& d;
+  int at, end;
+  __device__ __forceinline__ Walk(const Params& p_, const Lengths& s_, const Deal& d_, int cta) : p(p_), s(s_), d(d_) {
+    at = cta < d.n ? d.lo(cta) : 0;
+    end = cta < d.n ? d.lo(cta + 1) : 0;
+  }
+  __device__ __forceinline__ bool next(Segment& g) {
+    if (at >= end) return false;
+    int rest;
+    const int grp = d.group_of(at, rest);
+    g.b = element_of(s, p.batch, rest);
+    g.layer = p.by_kv_heads.divmod(grp, g.kvh);
+    g.Lc = s.lc[g.b];
+    g.Lq = s.lq[g.b];
+    const int unit = grp * d.sum + s.prefix[g.b];
+    g.begin = at - unit;
+    g.end = min(s.prefix[g.b + 1] - s.prefix[g.b], end - unit);
+    at = unit + g.end;
+    return true;
+  }
+};
+
+// Tiles begin, begin + 2, .. of a segment belong to group 0 of the warps, the others to group 1; tile i of a group (counted over the block's
+// life) has K stage 2 * group + (i & 1).  Every role enumerates the loads of query rows alike: events, event e in slot e & 1.  Up to two chunks:
+// one event each for a segment; more: one each for a pair of tiles.
+//
+// A wait for a barrier's phase works only when the phase before is over, so whoever waits on a barrier either has to arrive for its next
+// phase or waits behind something that does: hence stages that belong to one group, and events that each role takes, also where it has
+// no tile.
+template <int D, bool kQ4>
+__global__ void __launch_bounds__(kThreads, 1)
+cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ Params p) {
+  using G = Shape<D>;
+  using Pk = q4::Packed<D>;
+  constexpr int KS = G::KS, PS = G::PS;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t smem_pad = (1024u - (smem_u32(smem_raw) & 1023u)) & 1023u;
+  const uint32_t sm_q = smem_u32(smem_raw) + smem_pad, sm_k = sm_q + 2 * G::kTile, sm_p = sm_k + KS * G::kTile;
+  const uint32_t packed_bytes = kQ4 ? PS * G::kPackedStage : 0;
+  const uint32_t sm_log = sm_p + packed_bytes, sm_bar = sm_log + G::kLogBytes;
+  int* const flags = reinterpret_cast<int*>(smem_raw + smem_pad + G::kTiles + packed_bytes + G::kLogBytes + kBarrierBytes);
+  float* const logs = reinterpret_cast<float*>(smem_raw + smem_pad + G::kTiles + packed_bytes);
+  volatile int* const abort_ptr = flags;
+  volatile int* const never_ptr = flags + 1;
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(flags + 2);
+  const Lengths len(flags + kFlagBytes / 4, p.batch);
+
+  const uint32_t bar_k_full = sm_bar, bar_k_empty = bar_k_full + 8 * KS, bar_p_full = bar_k_empty + 8 * KS, bar_p_empty = bar_p_full + 8 * PS;
+  const uint32_t bar_q_tx = bar_p_empty + 8 * PS, bar_q_ready = bar_q_tx + 16, bar_q_empty = bar_q_ready + 16;   // [slot]
+  const uint32_t bar_s_ready = bar_q_empty + 16, bar_s_empty = bar_s_ready + 32;                                // [warp group][buffer]
+  const uint32_t bar_drain = bar_s_empty + 32;                                                                 // [2]
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    *abort_ptr = 0; *never_ptr = 0;
+    for (int i = 0; i < KS; ++i) {
+      mbar_init(bar_k_full + 8 * i, kQ4 ? kDecodeWarps : 1);
+      mbar_init(bar_k_empty + 8 * i, 1);
+    }
+    for (int i = 0; i < PS; ++i) {
+      mbar_init(bar_p_full + 8 * i, 1);
+      mbar_init(bar_p_empty + 8 * i, kDecodeWarps);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar_q_tx + 8 * i, 1);
+      mbar_init(bar_q_ready + 8 * i, 1);
+      mbar_init(bar_q_empty + 8 * i, 10);    // the warps that sum, the issuers
+      mbar_init(bar_drain + 8 * i, 1);
+    }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(bar_s_ready + 8 * i, 1);
+      mbar_init(bar_s_empty + 8 * i, 4);
+    }
+    mbar_fence_init();
+    fence_proxy_async_smem();
+  }
+  if (warp == 13) {
+    tmem_alloc(smem_u32(tmem_slot), kTmemCols);
+    tmem_relinquish();
+  }
+  if (warp == 12 && lane == 0) {
+    prefetch_tensormap(&tm_q);
+    if (!kQ4) prefetch_tensormap(&tm_k);
+  }
+  dlm_grid_dependency_wait();
+  dlm_trigger_dependents();
+  if (warp == 0)
+    read_lengths(p.cache_len, p.q_len, p.batch, p.capacity, p.q_cap, p.status, len, nullptr, [](int Lc, int) { return (Lc + kKeys - 1) / kKeys; });
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = *tmem_slot;
+  const Deal deal(len.prefix[p.batch], p.nl * p.n_kv_heads, (int)gridDim.x, 1);
+  const bool resident = p.n_qc <= 2;
+  auto chunk_rows = [&](int c) { return min(kRows, p.rows_total - c * kRows); };
+  Walk walk(p, len, deal, blockIdx.x);
+  Segment g = {};
+  bool ok = true;
+
+  if (warp == 12) {
+    if (lane == 0) {
+      // ================================================================= producer
+      uint32_t kt = 0, ev = 0, tiles[2] = {0, 0};   // packed tiles, events, tiles of the groups
+      auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait(bar, parity, abort_ptr); };
+      auto load_q = [&](int c) {
+        const uint32_t s = ev & 1;
+        if (ev >= 2 && !wait(bar_q_empty + 8 * s, ((ev >> 1) - 1) & 1)) return false;
+        mbar_expect_tx(bar_q_tx + 8 * s, (uint32_t)p.q_box * 128u * G::kPanels);   // a box counts in full
+        const int z = (g.layer * p.batch + g.b) * p.n_kv_heads + g.kvh;
+        for (int pn = 0; pn < G::kPanels; ++pn) tma_load_3d(sm_q + s * G::kTile + pn * G::kPanel, &tm_q, bar_q_tx + 8 * s, pn * 64, c * kRows, z);
+        ++ev;
+        return true;
+      };
+      auto load_k = [&](int t, int w) {
+        const int z = ((g.layer + p.layer_begin) * p.batch + g.b) * p.n_kv_heads + g.kvh;
+        if (kQ4) {
+          const uint32_t s = kt % PS, bar = bar_p_full + 8 * s, dst = sm_p + s * G::kPackedStage;
+          if (kt >= (uint32_t)PS && !wait(bar_p_empty + 8 * s, (kt / PS - 1) & 1)) return false;
+          const int rows = min(kKeys, g.Lc - t * kKeys), first = min(rows, 64), second = rows - first;
+          const size_t row = (size_t)z * p.capacity + (size_t)t * kKeys;
+          mbar_expect_tx(bar, Pk::bytes(first) + (second > 0 ? Pk::bytes(second) : 0u));
+          Pk::copy(dst, p.k, p.k_scale, row, first, bar);
+          if (second > 0) Pk::copy(dst + Pk::kBytes, p.k, p.k_scale, row + 64, second, bar);
+          ++kt;
+        } else {
+          const uint32_t i = tiles[w], s = 2 * w + (i & 1), bar = bar_k_full + 8 * s;
+          if (i >= 2 && !wait(bar_k_empty + 8 * s, ((i >> 1) - 1) & 1)) return false;
+          mbar_expect_tx(bar, (uint32_t)p.k_box * 128u * G::kPanels);
+          for (int pn = 0; pn < G::kPanels; ++pn) tma_load_3d(sm_k + s * G::kTile + pn * G::kPanel, &tm_k, bar, pn * 64, t * kKeys, z);
+          ++tiles[w];
+        }
+        return true;
+      };
+      while (ok && walk.next(g)) {
+        if (resident)
+          for (int c = 0; c < p.n_qc && ok; ++c) ok = load_q(c);
+        for (int t = g.begin; t < g.end && ok; t += 2) {
+          ok = load_k(t, 0);
+          if (ok && t + 1 < g.end) ok = load_k(t + 1, 1);
+          if (!resident)
+            for (int c = 0; c < p.n_qc && ok; ++c) ok = load_q(c);
+        }
+      }
+      // no copy lands after the block has released its shared memory
+      if (kQ4) {
+        for (uint32_t i = kt > (uint32_t)PS ? kt - PS : 0; i < kt; ++i) mbar_wait(bar_p_full + 8 * (i % PS), (i / PS) & 1, never_ptr);
+      } else {
+        for (int w = 0; w < 2; ++w)
+          for (uint32_t i = tiles[w] > 2 ? tiles[w] - 2 : 0; i < tiles[w]; ++i) mbar_wait(bar_k_full + 8 * (2 * w + (i & 1)), (i >> 1) & 1, never_ptr);
+      }
+      for (uint32_t i = ev > 2 ? ev - 2 : 0; i < ev; ++i) mbar_wait(bar_q_tx + 8 * (i & 1), (i >> 1) & 1, never_ptr);
+    }
+  } else if (warp == 13 || warp == 14) {
+    if (elect_one_sync()) {
+      // ================================================================= MMA issuers, one for each group of warps
+      const int w = warp - 13;
+      auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait(bar, parity, abort_ptr); };
+      uint32_t kt = 0, ev = 0, st = 0;   // the group's tiles, events, the group's steps so far
+      const uint64_t desc_k0 = make_smem_desc_sw128(sm_k, 16, 1024), desc_q0 = make_smem_desc_sw128(sm_q, 16, 1024);
+      auto take_event = [&](uint32_t e) { return wait(bar_q_ready + 8 * (e & 1), (e >> 1) & 1); };
+      while (ok && walk.next(g)) {
+        for (int t = g.begin + w; t - w < g.end && ok; t += 2) {
+          const bool mine = t < g.end;
+          const uint32_t ks = 2 * w + (kt & 1);
+          if (mine) ok = wait(bar_k_full + 8 * ks, (kt >> 1) & 1);
+          for (int c = 0; c < p.n_qc && ok && (mine || !resident); ++c) {
+            const uint32_t e = ev + c;
+            ok = take_event(e);
+            if (ok && mine) {
+              const uint32_t b = st & 1, buf = 16 * w + 8 * b;
+              ok = st < 2 || wait(bar_s_empty + buf, ((st >> 1) - 1) & 1);
+              if (!ok) break;
+              tc_fence_after_sync();
+              const uint32_t idesc = make_idesc_bf16(128, (uint32_t)((chunk_rows(c) + 15) & ~15), 0);
+              const uint64_t dk = desc_offset(desc_k0, ks * G::kTile), dq = desc_offset(desc_q0, (e & 1) * G::kTile);
+              const uint32_t d = tmem + w * 256 + b * kRows;
+#pragma unroll
+              for (int k = 0; k < D / 16; ++k) {
+                const uint32_t off = ((k >> 2) * G::kPanel + (k & 3) * 32) >> 4;
+                mma_ss_lo<false>(d, (uint32_t)dk + off, (uint32_t)dq + off, (uint32_t)(dk >> 32), idesc, k > 0 ? 1u : 0u);
+              }
+              tc_commit(bar_s_ready + buf);
+              ++st;
+            }
+            if (ok && !resident) mbar_arrive(bar_q_empty + 8 * (e & 1));   // (the slot is not free before the group's warps have summed this step)
+          }
+          if (ok && mine) {
+            tc_commit(bar_k_empty + 8 * ks);
+            ++kt;
+          }
+          if (!resident) ev += p.n_qc;
+        }
+        if (resident) {
+          for (int c = 0; c < p.n_qc && ok; ++c) {
+            ok = take_event(ev + c);
+            if (ok) mbar_arrive(bar_q_empty + 8 * ((ev + c) & 1));
+          }
+          ev += p.n_qc;
+        }
+      }
+      tc_commit(bar_drain + 8 * w);
+      mbar_wait(bar_drain + 8 * w, 0, never_ptr);
+    }
+  } else if (warp == 15) {
+    // ================================================================= query rows: logarithms, zeros
+    uint32_t ev = 0;
+    while (ok && walk.next(g)) {
+      const int events = resident ? p.n_qc : p.n_qc * ((g.end - g.begin + 1) / 2);
+      const float* const lse = p.lse + (((size_t)g.layer * p.batch + g.b) * p.n_q_heads + (size_t)g.kvh * p.group) * p.q_cap;
+      for (int i = 0, c = 0; i < events && ok; ++i, ++ev, c = c + 1 == p.n_qc ? 0 : c + 1) {
+        const uint32_t s = ev & 1;
+        const int n16 = (chunk_rows(c) + 15) & ~15;
+        float x[kRows / 32];
+        bool out[kRows / 32];
+#pragma unroll
+        for (int j = 0; j < kRows / 32; ++j) {
+          const int r = j * 32 + lane, r_kv = c * kRows + r;
+          const bool in = r_kv < p.rows_total && r_kv - p.by_q_cap.div(r_kv) * p.q_cap < g.Lq;
+          x[j] = in ? lse[r_kv] : -CUDART_INF_F;
+          out[j] = x[j] == -CUDART_INF_F;
+        }
+        // the copy into the slot shows that the slot's logarithms have been used too
+        ok = mbar_wait_warp(bar_q_tx + 8 * s, (ev >> 1) & 1, abort_ptr);
+        if (!ok) break;
+#pragma unroll
+        for (int j = 0; j < kRows / 32; ++j) {
+          const int r = j * 32 + lane;
+          logs[s * kRows + r] = out[j] ? -CUDART_INF_F : x[j] * -1.4426950408889634f;
+          // a row that takes no part: 0 * scale - inf, whatever it holds
+          for (uint32_t todo = __ballot_sync(0xffffffffu, out[j] && r < n16); todo != 0; todo &= todo - 1)
+            if (lane < D / 8) q4::clear_piece<D>(sm_q + s * G::kTile, G::kPanel, (j * 32 + __ffs(todo) - 1) * (D / 8) + lane);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_q_ready + 8 * s);
+      }
+    }
+  } else if (warp >= 8) {
+    if (kQ4) {
+      // ================================================================= decoders
+      constexpr int kGroups = D / q4::kGroup, kPer = kKeys * kGroups / (kDecodeWarps * 32);
+      const int me = tid - 256;
+      uint32_t kt = 0, tiles[2] = {0, 0};
+      while (ok && walk.next(g)) {
+        for (int t = g.begin; t < g.end && ok; ++t, ++kt) {
+          const int w = (t - g.begin) & 1;
+          const uint32_t n = w ? tiles[1]++ : tiles[0]++;
+          const uint32_t s = kt % PS, ks = 2 * w + (n & 1), packed = sm_p + s * G::kPackedStage, tile = sm_k + ks * G::kTile;
+          ok = mbar_wait_warp(bar_p_full + 8 * s, (kt / PS) & 1, abort_ptr);
+          if (!ok) break;
+          const int tasks = min(kKeys, g.Lc - t * kKeys) * kGroups;
+          q4::Group32 x[kPer];
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) {
+            const int task = me + i * kDecodeWarps * 32, half = task / (64 * kGroups);
+            if (task < tasks) x[i] = q4::read_group<D>(packed + half * Pk::kBytes, task - half * 64 * kGroups);
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar_p_empty + 8 * s);
+          if (n >= 2) ok = mbar_wait_warp(bar_k_empty + 8 * ks, ((n >> 1) - 1) & 1, abort_ptr);
+          if (!ok) break;
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) {
+            const int task = me + i * kDecodeWarps * 32;
+            if (task < tasks) q4::write_group<D>(tile, G::kPanel, task, x[i]);
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar_k_full + 8 * ks);
+        }
+      }
+    }
+  } else {
+    // ================================================================= sums: thread = key of the tile = TMEM lane
+    const int w = warp >> 2, key = (warp & 3) * 32 + lane;
+    const uint32_t t_s = tmem + ((uint32_t)((warp & 3) * 32) << 16) + w * 256;
+    const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2);
+    uint32_t ev = 0, st = 0;
+    while (ok && walk.next(g)) {
+      const size_t row0 = (((size_t)(g.layer + p.layer_begin) * p.batch + g.b) * p.n_kv_heads + g.kvh) * p.capacity;
+      for (int t0 = g.begin; t0 < g.end && ok; t0 += 2) {
+        const int t = t0 + w;
+        if (t < g.end) {
+          float a0 = 0.f, a1 = 0.f, a2 = 0.f, a3 = 0.f;
+          const int j = t * kKeys + key;
+          const float before = j < g.Lc && p.collected && p.decay != 0.f ? p.decay * p.collected[row0 + j] : 0.f;
+          for (int c = 0; c < p.n_qc && ok; ++c, ++st) {
+            const uint32_t e = ev + c, b = st & 1, buf = 16 * w + 8 * b;
+            const int n16 = (chunk_rows(c) + 15) & ~15;
+            ok = mbar_wait_warp(bar_s_ready + buf, (st >> 1) & 1, abort_ptr);   // (behind q_ready, whose logarithms are read here)
+            if (ok) ok = mbar_wait_warp(bar_q_ready + 8 * (e & 1), (e >> 1) & 1, abort_ptr);
+            if (!ok) break;
+            tc_fence_after_sync();
+            const uint32_t from = t_s + b * kRows, log_at = sm_log + (e & 1) * kRows * 4;
+            auto add = [&](const uint32_t* v, uint32_t at, int n) {
+#pragma unroll
+              for (int i = 0; i < 32; i += 4) {
+                if (i >= n) break;
+                const float4 l = ld_shared_f4(at + i * 4);
+                float x0, x1, x2, x3;
+                unpack2(fma2(pack2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), scale2, pack2(l.x, l.y)), x0, x1);
+                unpack2(fma2(pack2(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])), scale2, pack2(l.z, l.w)), x2, x3);
+                a0 += ex2_approx(x0);
+                a1 += ex2_approx(x1);
+                a2 += ex2_approx(x2);
+                a3 += ex2_approx(x3);
+              }
+            };
+            uint32_t v[32];
+#pragma unroll 1
+            for (int i = 0; i + 32 <= n16; i += 32) {
+              tmem_ld32(from + i, v);
+              tmem_ld_wait();
+              add(v, log_at + i * 4, 32);
+            }
+            if (n16 & 16) {
+              tmem_ld16(from + (n16 & ~31), v);
+              tmem_ld_wait();
+              add(v, log_at + (n16 & ~31) * 4, 16);
+            }
+            __syncwarp();
+            if (lane == 0) {
+              tc_fence_before_sync();
+              mbar_arrive(bar_s_empty + buf);
+              if (!resident) mbar_arrive(bar_q_empty + 8 * (e & 1));
+            }
+          }
+          if (ok && j < g.Lc) p.weight[row0 + j] = before + ((a0 + a1) + (a2 + a3));
+        } else if (!resident) {   // no second tile: the query rows are not needed here
+          for (int c = 0; c < p.n_qc && ok; ++c) {
+            ok = mbar_wait_warp(bar_q_ready + 8 * ((ev + c) & 1), ((ev + c) >> 1) & 1, abort_ptr);
+            __syncwarp();
+            if (ok && lane == 0) mbar_arrive(bar_q_empty + 8 * ((ev + c) & 1));
+          }
+        }
+        if (!resident) ev += p.n_qc;
+      }
+      if (resident) {
+        for (int c = 0; c < p.n_qc && ok; ++c) {
+          ok = mbar_wait_warp(bar_q_ready + 8 * ((ev + c) & 1), ((ev + c) >> 1) & 1, abort_ptr);
+          __syncwarp();
+          if (ok && lane == 0) mbar_arrive(bar_q_empty + 8 * ((ev + c) & 1));
+        }
+        ev += p.n_qc;
+      }
+    }
+  }
+  // ---- teardown
+  __syncwarp();
+  tc_fence_before_sync();
+  __syncthreads();
+  if (tid == 0 && (*abort_ptr || *never_ptr)) dlm_set_status(p.status, DLM_ERR_TIMEOUT);
+  if (warp == 13) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, kTmemCols);
+    __syncwarp();
+  }
+}
+
+using Kernel = void (*)(const CUtensorMap, const CUtensorMap, const Params);
+
+template <bool kQ4, typename Cache>
+int accumulate(dlm_ctx* ctx, const Cache* cache, const uint8_t* k_scale, int layer_begin, int layer_end, const void* q, const float* lse,
+               int n_q_heads, int q_cap, const int32_t* q_len, float softmax_scale, const float* collected, float decay, float* weight,
+               void* stream) {
+  if (n_q_heads <= 0 || q_cap <= 0 || layer_begin < 0 || layer_end > cache->n_layers || layer_begin >= layer_end) return DLM_ERR_SHAPE;
+  const int D = cache->head_dim;
+  if ((D != 64 && D != 128) || n_q_heads % cache->n_kv_heads != 0 || decay != decay) return DLM_ERR_UNSUPPORTED;
+  const int group = n_q_heads / cache->n_kv_heads, nl = layer_end - layer_begin;
+  if (q_cap > kMaxQCap || (long long)group * q_cap > (1 << 20) || cache->batch > kMaxBatch) return DLM_ERR_UNSUPPORTED;
+  if (((uintptr_t)q | (uintptr_t)cache->k) & 15) return DLM_ERR_UNSUPPORTED;
+  const long long units = (long long)nl * cache->batch * cache->n_kv_heads, tiles = (cache->capacity + kKeys - 1) / kKeys;
+  if (units * tiles >= (1LL << 30)) return DLM_ERR_UNSUPPORTED;   // items are counted in 32 bits
+  DLM_DEVICE_TRY(ctx);
+  const Kernel kern = D == 128 ? cache_weight_kernel<128, kQ4> : cache_weight_kernel<64, kQ4>;
+  const int which = (D == 128 ? 0 : 1) + (kQ4 ? 2 : 0);
+  if (ctx->weight_smem_limit[which] == 0) {
+    DLM_CUDA_TRY(cudaFuncSetAttribute(reinterpret_cast<const void*>(kern), cudaFuncAttributeMaxDynamicSharedMemorySize, ctx->max_smem_optin));
+    ctx->weight_smem_limit[which] = ctx->max_smem_optin;
+  }
+  const int tiles_bytes = D == 128 ? Shape<128>::kTiles + (kQ4 ? Shape<128>::PS * Shape<128>::kPackedStage : 0)
+                                   : Shape<64>::kTiles + (kQ4 ? Shape<64>::PS * Shape<64>::kPackedStage : 0);
+  const int smem = 1024 + tiles_bytes + Shape<64>::kLogBytes + kBarrierBytes + kFlagBytes + 4 * length_ints(cache->batch);
+  if (smem > ctx->max_smem_optin) return DLM_ERR_UNSUPPORTED;
+  Params p;
+  p.cache_len = cache->cache_len;
+  p.q_len = q_len;
+  p.k = static_cast<const uint8_t*>(cache->k);
+  p.k_scale = k_scale;
+  p.lse = lse;
+  p.collected = collected;
+  p.weight = weight;
+  p.decay = decay;
+  p.nl = nl;
+  p.layer_begin = layer_begin;
+  p.batch = cache->batch;
+  p.n_kv_heads = cache->n_kv_heads;
+  p.n_q_heads = n_q_heads;
+  p.group = group;
+  p.capacity = cache->capacity;
+  p.q_cap = q_cap;
+  p.rows_total = group * q_cap;
+  p.n_qc = (p.rows_total + kRows - 1) / kRows;
+  p.q_box = p.rows_total < kRows ? p.rows_total : kRows;
+  p.k_box = cache->capacity < kKeys ? cache->capacity : kKeys;
+  p.by_kv_heads = make_fast_div(p.n_kv_heads);
+  p.by_q_cap = make_fast_div(q_cap);
+  p.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;
+  p.status = &ctx->words->status;
+  CUtensorMap tm_q, tm_k;
+  int rc = encode_rows_map(ctx, &tm_q, q, D, p.rows_total, (long long)nl * cache->batch * cache->n_kv_heads, p.q_box);
+  tm_k = tm_q;
+  if (!kQ4 && rc == DLM_OK)
+    rc = encode_rows_map(ctx, &tm_k, cache->k, D, cache->capacity, (long long)cache->n_layers * cache->batch * cache->n_kv_heads, p.k_box);
+  if (rc != DLM_OK) return rc;
+  const int sms = ctx->num_sms < kMaxGrid ? ctx->num_sms : kMaxGrid, grid = units * tiles < sms ? (int)(units * tiles) : sms;
+  DLM_CUDA_TRY(dlm_launch(kern, dim3(grid), dim3(kThreads), (size_t)smem, static_cast<cudaStream_t>(stream), tm_q, tm_k, p));
+  return dlm_launch_ok(ctx, 1);
+}
+
+}  // namespace
+
+extern "C" int dlm_cache_weight_accumulate(dlm_ctx* ctx, const dlm_kv_cache* cache, int layer_begin, int layer_end, const void* q,
+                                           const float* lse, int n_q_heads, int q_cap, const int32_t* q_len, float softmax_scale,
+                                           int cache_len_hint, const float* collected, float decay, float* weight, void* stream) {
+  (void)cache_len_hint;
+  if (!ctx || !cache || !cache->k || !cache->cache_len || !q || !lse || !weight) return DLM_ERR_NULL;
+  if (cache->n_layers <= 0 || cache->batch <= 0 || cache->n_kv_heads <= 0 || cache->capacity <= 0) return DLM_ERR_SHAPE;
+  return accumulate<false>(ctx, cache, nullptr, layer_begin, layer_end, q, lse, n_q_heads, q_cap, q_len, softmax_scale, collected, decay,
+                           weight, stream);
+}
+
+extern "C" int dlm_cache_weight_accumulate_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* cache, int layer_begin, int layer_end, const void* q,
+                                              const float* lse, int n_q_heads, int q_cap, const int32_t* q_len, float softmax_scale,
+                                              int cache_len_hint, const float* collected, float decay, float* weight, void* stream) {
+  (void)cache_len_hint;
+  if (!ctx || !q || !lse || !weight) return DLM_ERR_NULL;
+  const int bad = dlm_check_q4(cache);
+  if (bad != DLM_OK) return bad;
+  return accumulate<true>(ctx, cache, static_cast<const uint8_t*>(cache->k_scale), layer_begin, layer_end, q, lse, n_q_heads, q_cap, q_len,
+                          softmax_scale, collected, decay, weight, stream);
+}

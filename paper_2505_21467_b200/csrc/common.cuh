@@ -55,7 +55,7 @@ struct dlm_ctx {
   void* encode_tiled;       // cuTensorMapEncodeTiled and cuTensorMapReplaceAddress (driver API), resolved lazily
   void* replace_address;
   dlm_map_cache* maps;
-  int commit_blocks_per_sm[2];  // resident blocks per SM of the two commit kernels (0 = not asked yet)
+  int commit_blocks_per_sm[4];  // resident blocks per SM of the commit kernels (0 = not asked yet)
   unsigned long long wait_limit_ns;   // limit of the kernels' device-side waits (2 s; a test may shorten it)
   unsigned int proj_configured; // bit per projection kernel: shared-memory opt-in done on this context's device
   int attn_team_max;            // most blocks the attention call's team schedule may give one unit (1 = schedule off)
@@ -64,6 +64,8 @@ struct dlm_ctx {
   dlm_attn_plan attn_plan;
   int attn_clusters[17];        // clusters of so many attention blocks that the device runs at a time (0 = not asked yet, -1 = none)
   int attn_smem_limit[32];      // dynamic shared memory the attention kernels may use on this device (0 = not set up yet)
+  int q4_smem_limit[8];         // ... those of the 4-bit cache
+  int weight_smem_limit[4];     // ... the kernels that accumulate weights
 };
 
 // Writes the descriptor of a bf16 tensor of `rank` dimensions (sizes, byte strides of dimensions 1 .., box), 128-byte swizzle,
@@ -154,6 +156,15 @@ static inline int dlm_check_device(const dlm_ctx* ctx) {
     const int _d = dlm_check_device(ctx);          \
     if (_d != DLM_OK) return _d;                   \
   } while (0)
+
+// What every call on a 4-bit cache asks of it.  A head's rows of scales then start on 16 bytes (capacity a multiple of 8).
+static inline int dlm_check_q4(const dlm_kv_cache_q4* c) {
+  if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale || !c->cache_len) return DLM_ERR_NULL;
+  if (c->n_layers <= 0 || c->batch <= 0 || c->n_kv_heads <= 0 || c->capacity <= 0 || c->head_dim <= 0) return DLM_ERR_SHAPE;
+  if ((c->head_dim != 64 && c->head_dim != 128) || c->capacity % 8 != 0) return DLM_ERR_UNSUPPORTED;
+  if (((uintptr_t)c->k | (uintptr_t)c->v | (uintptr_t)c->k_scale | (uintptr_t)c->v_scale) & 15) return DLM_ERR_UNSUPPORTED;
+  return DLM_OK;
+}
 
 static inline int dlm_launch_ok(dlm_ctx* ctx, int n_kernels) {
   if (cudaGetLastError() != cudaSuccess) return DLM_ERR_CUDA;

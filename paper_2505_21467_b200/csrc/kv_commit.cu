@@ -1,5 +1,6 @@
 // dlm_kv_cache_commit: row gather/scatter of fresh K/V into the device-resident cache
-// (Sec. 3.2.1: saving K/V at initialisation, freezing a finished block).
+// (Sec. 3.2.1: saving K/V at initialisation, freezing a finished block); dlm_kv_cache_commit_q4, the same into a cache of 4
+// bits, and dlm_kv_cache_read_q4, rows of that cache back as bf16.
 //
 // Pure data movement, bound by HBM.  One work item is one 16-byte vector of one K row and
 // the matching vector of the V row; items are ordered [layer][batch][head][row][vector] so
@@ -10,6 +11,7 @@
 // decoded with 32-bit reciprocals whenever the call has fewer than 2^31 items (64-bit divisions
 // by run-time divisors cost more than the copy).  The last block to finish advances cache_len.
 #include "common.cuh"
+#include "q4.cuh"
 
 namespace {
 
@@ -17,8 +19,10 @@ constexpr int kThreads = 256;
 constexpr int kUnroll = 4;
 
 struct CommitParams {
-  uint4* cache_k;
-  uint4* cache_v;
+  void* cache_k;         // 16-byte vectors; 4-bit cache: a 32-bit word for each vector of a source row
+  void* cache_v;
+  uint8_t* k_scale;      // 4-bit cache: a byte for every fourth
+  uint8_t* v_scale;
   int32_t* cache_len;
   const uint4* k_new;
   const uint4* v_new;
@@ -108,18 +112,41 @@ __device__ __forceinline__ void advance_when_last(const CommitParams& p) {
   if (threadIdx.x == 0) *p.ticket = 0;
 }
 
-template <typename Idx>
+// The vectors kk and vv to where `to` says (vector number in the cache, -1: nowhere).  4-bit cache: four neighbouring lanes have a
+// group of 32 values, which lies in one row (a row's vectors are a multiple of four), so all four have a destination or none has;
+// every lane of the warp calls this.
+template <bool kQ4>
+__device__ __forceinline__ void store_rows(const CommitParams& p, long long to, const uint4& kk, const uint4& vv) {
+  if (kQ4) {
+    uint32_t kb, vb;
+    const uint32_t kw = q4::encode8(kk, kb), vw = q4::encode8(vv, vb);
+    if (to < 0) return;
+    static_cast<uint32_t*>(p.cache_k)[to] = kw;
+    static_cast<uint32_t*>(p.cache_v)[to] = vw;
+    if ((to & 3) == 0) {
+      p.k_scale[to >> 2] = (uint8_t)kb;
+      p.v_scale[to >> 2] = (uint8_t)vb;
+    }
+  } else if (to >= 0) {
+    static_cast<uint4*>(p.cache_k)[to] = kk;
+    static_cast<uint4*>(p.cache_v)[to] = vv;
+  }
+}
+
+template <typename Idx, bool kQ4>
 __global__ void __launch_bounds__(kThreads, 4) kv_commit_kernel(const __grid_constant__ CommitParams p) {
   dlm_grid_dependency_wait();
   dlm_trigger_dependents();
   const Idx begin = (Idx)blockIdx.x * (Idx)p.per_block;
   const Idx end = (Idx)min((long long)begin + p.per_block, p.n_items);
-  for (Idx base = begin + (Idx)threadIdx.x; base < end; base += (Idx)(kThreads * kUnroll)) {
+  // (4 bits: the lanes of a warp leave together)
+  for (Idx base = begin + (Idx)threadIdx.x; kQ4 ? (base & ~(Idx)31) < end : base < end; base += (Idx)(kThreads * kUnroll)) {
     uint4 kk[kUnroll], vv[kUnroll];
     long long to[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       to[u] = -1;
+      if (kQ4) kk[u] = vv[u] = make_uint4(0, 0, 0, 0);
       const Idx item = base + (Idx)(u * kThreads);
       if (item >= end) continue;
       const Move mv = find_move<Idx>(p, item);
@@ -130,12 +157,7 @@ __global__ void __launch_bounds__(kThreads, 4) kv_commit_kernel(const __grid_con
       }
     }
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      if (to[u] >= 0) {
-        p.cache_k[to[u]] = kk[u];
-        p.cache_v[to[u]] = vv[u];
-      }
-    }
+    for (int u = 0; u < kUnroll; ++u) store_rows<kQ4>(p, to[u], kk[u], vv[u]);
   }
   if (p.advance_len) advance_when_last(p);
 }
@@ -144,6 +166,7 @@ __global__ void __launch_bounds__(kThreads, 4) kv_commit_kernel(const __grid_con
 // advance_len also ticket and lengths, which go beside the row's): four items a thread put four decodings in front of the
 // first load, and the ticket behind the stores (28 layers x 4 rows: 3.9 us; 8 x 32 rows with advance_len 3.9 us;
 // now 1.9 and 1.8).
+template <bool kQ4>
 __global__ void __launch_bounds__(kThreads) kv_commit_small_kernel(const __grid_constant__ CommitParams p) {
   dlm_grid_dependency_wait();
   dlm_trigger_dependents();
@@ -156,30 +179,104 @@ __global__ void __launch_bounds__(kThreads) kv_commit_small_kernel(const __grid_
     vv = __ldcs(p.v_new + mv.from);
   }
   if (p.advance_len) advance_when_last(p);
-  if (mv.to >= 0) {
-    p.cache_k[mv.to] = kk;
-    p.cache_v[mv.to] = vv;
+  store_rows<kQ4>(p, mv.to, kk, vv);
+}
+
+// Rows of the 4-bit cache as bf16: one item is 8 values of a K row and of the V row, a 32-bit word and a scale byte each.  Bound by HBM
+// like the commit; items, decoding and the words' coalescing are the commit's.
+struct ReadParams {
+  const uint32_t* k;
+  const uint32_t* v;
+  const uint8_t* k_scale;
+  const uint8_t* v_scale;
+  const int32_t* src_pos;
+  const int32_t* n_rows;
+  uint4* k_out;
+  uint4* v_out;
+  int n_max, layer_begin, batch, n_kv_heads, capacity, vec_per_row;
+  FastDiv by_vec, by_rows, by_heads, by_batch;
+  long long n_items;
+  int* status;
+};
+
+template <typename Idx>
+__global__ void __launch_bounds__(kThreads) kv_read_q4_kernel(const __grid_constant__ ReadParams p) {
+  dlm_grid_dependency_wait();
+  dlm_trigger_dependents();
+  const Idx step = (Idx)gridDim.x * kThreads;
+  for (Idx base = (Idx)blockIdx.x * kThreads + (Idx)threadIdx.x; base < (Idx)p.n_items; base += step * kUnroll) {
+    uint32_t kw[kUnroll], vw[kUnroll], kb[kUnroll], vb[kUnroll];
+    bool on[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const Idx item = base + (Idx)u * step;
+      on[u] = item < (Idx)p.n_items;
+      if (!on[u]) continue;
+      int vec, r, h, b, lc;
+      if (sizeof(Idx) == 4) {
+        lc = p.by_batch.divmod(p.by_heads.divmod(p.by_rows.divmod(p.by_vec.divmod((int)item, vec), r), h), b);
+      } else {
+        long long rest = (long long)item;
+        vec = (int)(rest % p.vec_per_row);
+        rest /= p.vec_per_row;
+        r = (int)(rest % p.n_max);
+        rest /= p.n_max;
+        h = (int)(rest % p.n_kv_heads);
+        rest /= p.n_kv_heads;
+        b = (int)(rest % p.batch);
+        lc = (int)(rest / p.batch);
+      }
+      const int n = p.n_rows ? p.n_rows[b] : p.n_max;
+      const int row = p.src_pos ? p.src_pos[(long long)b * p.n_max + r] : r;
+      const bool first = vec == 0 && h == 0 && lc == 0;
+      if (n < 0 || n > p.n_max) {
+        if (first && r == 0) dlm_set_status(p.status, DLM_ERR_CAPACITY);
+        on[u] = false;
+      } else if (r >= n) {
+        on[u] = false;
+      } else if (row < 0 || row >= p.capacity) {
+        if (first) dlm_set_status(p.status, DLM_ERR_INDEX);
+        on[u] = false;
+      }
+      if (!on[u]) continue;
+      const long long at = ((((long long)(lc + p.layer_begin) * p.batch + b) * p.n_kv_heads + h) * p.capacity + row) * p.vec_per_row + vec;
+      kw[u] = p.k[at];
+      vw[u] = p.v[at];
+      kb[u] = p.k_scale[at >> 2];
+      vb[u] = p.v_scale[at >> 2];
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      if (!on[u]) continue;
+      const Idx item = base + (Idx)u * step;
+      uint32_t w[4];
+      q4::decode8(kw[u], q4::make_scale(kb[u]), w);
+      p.k_out[item] = make_uint4(w[0], w[1], w[2], w[3]);
+      q4::decode8(vw[u], q4::make_scale(vb[u]), w);
+      p.v_out[item] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
   }
 }
 
-}  // namespace
-
-extern "C" int dlm_kv_cache_commit(dlm_ctx* ctx, const dlm_kv_cache* cache, const void* k_new,
-                                   const void* v_new, int src_len, const int32_t* src_idx,
-                                   const int32_t* dst_pos, int dst_mode, const int32_t* n_rows, int n_max,
-                                   int advance_len, int layer_begin, int layer_end, void* stream) {
-  if (!ctx || !cache || !cache->k || !cache->v || !cache->cache_len || !k_new || !v_new) return DLM_ERR_NULL;
+// The arguments that the two commits share, checked; cache->k and ->v in vectors of 8 values.
+template <bool kQ4, typename Cache>
+int commit(dlm_ctx* ctx, const Cache* cache, uint8_t* k_scale, uint8_t* v_scale, const void* k_new, const void* v_new, int src_len,
+           const int32_t* src_idx, const int32_t* dst_pos, int dst_mode, const int32_t* n_rows, int n_max, int advance_len,
+           int layer_begin, int layer_end, void* stream) {
   if (cache->n_layers <= 0 || cache->batch <= 0 || cache->n_kv_heads <= 0 || cache->capacity <= 0 ||
       cache->head_dim <= 0 || src_len <= 0 || n_max <= 0 || (dst_mode != DLM_DST_APPEND && dst_mode != DLM_DST_WINDOW))
     return DLM_ERR_SHAPE;
   if (layer_begin < 0 || layer_end > cache->n_layers || layer_begin >= layer_end) return DLM_ERR_SHAPE;
-  if ((cache->head_dim * 2) % 16 != 0) return DLM_ERR_UNSUPPORTED;
+
+  if (kQ4 ? cache->head_dim % q4::kGroup != 0 : (cache->head_dim * 2) % 16 != 0) return DLM_ERR_UNSUPPORTED;
   if (((uintptr_t)cache->k | (uintptr_t)cache->v | (uintptr_t)k_new | (uintptr_t)v_new) & 15) return DLM_ERR_UNSUPPORTED;
   DLM_DEVICE_TRY(ctx);
 
   CommitParams p;
-  p.cache_k = static_cast<uint4*>(cache->k);
-  p.cache_v = static_cast<uint4*>(cache->v);
+  p.cache_k = cache->k;
+  p.cache_v = cache->v;
+  p.k_scale = k_scale;
+  p.v_scale = v_scale;
   p.cache_len = cache->cache_len;
   p.k_new = static_cast<const uint4*>(k_new);
   p.v_new = static_cast<const uint4*>(v_new);
@@ -206,11 +303,11 @@ extern "C" int dlm_kv_cache_commit(dlm_ctx* ctx, const dlm_kv_cache* cache, cons
 
   // one resident wave of equal contiguous ranges, or one item per thread where that is no more
   const bool narrow = p.n_items < (1LL << 31) - (long long)kThreads * kUnroll;
-  int& per_sm = ctx->commit_blocks_per_sm[narrow ? 0 : 1];
+  int& per_sm = ctx->commit_blocks_per_sm[(kQ4 ? 2 : 0) + (narrow ? 0 : 1)];
   if (per_sm <= 0) {
     int n = 0;
-    const cudaError_t e = narrow ? cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kv_commit_kernel<int>, kThreads, 0)
-                                 : cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kv_commit_kernel<long long>, kThreads, 0);
+    const cudaError_t e = narrow ? cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kv_commit_kernel<int, kQ4>, kThreads, 0)
+                                 : cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kv_commit_kernel<long long, kQ4>, kThreads, 0);
     if (e != cudaSuccess || n <= 0) return DLM_ERR_CUDA;
     per_sm = n;
   }
@@ -218,7 +315,7 @@ extern "C" int dlm_kv_cache_commit(dlm_ctx* ctx, const dlm_kv_cache* cache, cons
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (p.n_items <= max_blocks * kThreads) {
     const unsigned int blocks = (unsigned int)((p.n_items + kThreads - 1) / kThreads);
-    DLM_CUDA_TRY(dlm_launch(kv_commit_small_kernel, dim3(blocks), dim3(kThreads), 0, st, p));
+    DLM_CUDA_TRY(dlm_launch(kv_commit_small_kernel<kQ4>, dim3(blocks), dim3(kThreads), 0, st, p));
     return dlm_launch_ok(ctx, 1);
   }
   const long long per_pass = (long long)kThreads * kUnroll;
@@ -227,8 +324,72 @@ extern "C" int dlm_kv_cache_commit(dlm_ctx* ctx, const dlm_kv_cache* cache, cons
   p.per_block = ((p.n_items + blocks - 1) / blocks + 31) & ~31LL;
   blocks = (p.n_items + p.per_block - 1) / p.per_block;
   if (narrow)
-    DLM_CUDA_TRY(dlm_launch(kv_commit_kernel<int>, dim3((unsigned)blocks), dim3(kThreads), 0, st, p));
+    DLM_CUDA_TRY(dlm_launch(kv_commit_kernel<int, kQ4>, dim3((unsigned)blocks), dim3(kThreads), 0, st, p));
   else
-    DLM_CUDA_TRY(dlm_launch(kv_commit_kernel<long long>, dim3((unsigned)blocks), dim3(kThreads), 0, st, p));
+    DLM_CUDA_TRY(dlm_launch(kv_commit_kernel<long long, kQ4>, dim3((unsigned)blocks), dim3(kThreads), 0, st, p));
+  return dlm_launch_ok(ctx, 1);
+}
+
+}  // namespace
+
+extern "C" int dlm_kv_cache_commit(dlm_ctx* ctx, const dlm_kv_cache* cache, const void* k_new,
+                                   const void* v_new, int src_len, const int32_t* src_idx,
+                                   const int32_t* dst_pos, int dst_mode, const int32_t* n_rows, int n_max,
+                                   int advance_len, int layer_begin, int layer_end, void* stream) {
+  if (!ctx || !cache || !cache->k || !cache->v || !cache->cache_len || !k_new || !v_new) return DLM_ERR_NULL;
+  return commit<false>(ctx, cache, nullptr, nullptr, k_new, v_new, src_len, src_idx, dst_pos, dst_mode, n_rows, n_max, advance_len,
+                       layer_begin, layer_end, stream);
+}
+
+extern "C" int dlm_kv_cache_commit_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* cache, const void* k_new,
+                                      const void* v_new, int src_len, const int32_t* src_idx,
+                                      const int32_t* dst_pos, int dst_mode, const int32_t* n_rows, int n_max,
+                                      int advance_len, int layer_begin, int layer_end, void* stream) {
+  if (!ctx || !k_new || !v_new) return DLM_ERR_NULL;
+  const int rc = dlm_check_q4(cache);
+  if (rc != DLM_OK) return rc;
+  return commit<true>(ctx, cache, static_cast<uint8_t*>(cache->k_scale), static_cast<uint8_t*>(cache->v_scale), k_new, v_new, src_len,
+                      src_idx, dst_pos, dst_mode, n_rows, n_max, advance_len, layer_begin, layer_end, stream);
+}
+
+extern "C" int dlm_kv_cache_read_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* cache, const int32_t* src_pos, const int32_t* n_rows,
+                                    int n_max, int layer_begin, int layer_end, void* k_out, void* v_out, void* stream) {
+  if (!ctx || !k_out || !v_out) return DLM_ERR_NULL;
+  const int rc = dlm_check_q4(cache);
+  if (rc != DLM_OK) return rc;
+  if (n_max <= 0 || layer_begin < 0 || layer_end > cache->n_layers || layer_begin >= layer_end) return DLM_ERR_SHAPE;
+  if (!src_pos && n_max > cache->capacity) return DLM_ERR_SHAPE;
+  if (((uintptr_t)k_out | (uintptr_t)v_out) & 15) return DLM_ERR_UNSUPPORTED;
+  DLM_DEVICE_TRY(ctx);
+  ReadParams p;
+  p.k = static_cast<const uint32_t*>(cache->k);
+  p.v = static_cast<const uint32_t*>(cache->v);
+  p.k_scale = static_cast<const uint8_t*>(cache->k_scale);
+  p.v_scale = static_cast<const uint8_t*>(cache->v_scale);
+  p.src_pos = src_pos;
+  p.n_rows = n_rows;
+  p.k_out = static_cast<uint4*>(k_out);
+  p.v_out = static_cast<uint4*>(v_out);
+  p.n_max = n_max;
+  p.layer_begin = layer_begin;
+  p.batch = cache->batch;
+  p.n_kv_heads = cache->n_kv_heads;
+  p.capacity = cache->capacity;
+  p.vec_per_row = cache->head_dim / 8;
+  p.by_vec = make_fast_div(p.vec_per_row);
+  p.by_rows = make_fast_div(n_max);
+  p.by_heads = make_fast_div(cache->n_kv_heads);
+  p.by_batch = make_fast_div(cache->batch);
+  p.n_items = (long long)(layer_end - layer_begin) * p.batch * p.n_kv_heads * n_max * p.vec_per_row;
+  p.status = &ctx->words->status;
+  long long blocks = (p.n_items + kThreads - 1) / kThreads;
+  if (blocks > 8LL * ctx->num_sms) blocks = 8LL * ctx->num_sms;
+  // item numbers run up to n_items + kUnroll - 1 steps of the grid
+  const bool narrow = p.n_items + (kUnroll + 1) * blocks * kThreads < (1LL << 31);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (narrow)
+    DLM_CUDA_TRY(dlm_launch(kv_read_q4_kernel<int>, dim3((unsigned)blocks), dim3(kThreads), 0, st, p));
+  else
+    DLM_CUDA_TRY(dlm_launch(kv_read_q4_kernel<long long>, dim3((unsigned)blocks), dim3(kThreads), 0, st, p));
   return dlm_launch_ok(ctx, 1);
 }

@@ -14,9 +14,9 @@
 namespace {
 
 PyObject* g_error = nullptr;   // DlmError(code, where), set by the package
-// The classes whose memory is read as a pointer and as a dlm_kv_cache (ctypes.c_void_p and the package's structure), set by
+// The classes whose memory is read as a pointer, a dlm_kv_cache and a dlm_kv_cache_q4 (ctypes.c_void_p and the package's structures), set by
 // the package.  Nothing else will do: the bytes of another object would be taken for device addresses.
-PyTypeObject *g_handle_type = nullptr, *g_cache_type = nullptr;
+PyTypeObject *g_handle_type = nullptr, *g_cache_type = nullptr, *g_cache_q4_type = nullptr;
 
 struct Args;
 typedef int (*CallFn)(Args&);
@@ -67,6 +67,7 @@ struct Args {
     return p;
   }
   const dlm_kv_cache* cache(int i) { return static_cast<const dlm_kv_cache*>(buffer(i, g_cache_type, sizeof(dlm_kv_cache))); }
+  const dlm_kv_cache_q4* cache_q4(int i) { return static_cast<const dlm_kv_cache_q4*>(buffer(i, g_cache_q4_type, sizeof(dlm_kv_cache_q4))); }
   int integer(int i) {
     if (failed) return 0;
     if (PyLong_Check(v[i])) return (int)PyLong_AsUnsignedLongMask(v[i]);
@@ -312,6 +313,79 @@ int call_out(Args& a) {
   RELEASED(dlm_window_out_project(ctx, o, wo, bias, batch, q_cap, dm, hq, d, y, ws, bytes, s));
 }
 
+int call_commit_q4(Args& a) {
+  dlm_ctx* ctx = static_cast<dlm_ctx*>(a.handle(0));
+  const dlm_kv_cache_q4* cache = a.cache_q4(1);
+  const void *k = a.bf16(2), *v = a.bf16(3);
+  const int src_len = a.integer(4);
+  const int32_t *src_idx = a.i32(5), *dst_pos = a.i32(6);
+  const int dst_mode = a.integer(7);
+  const int32_t* n_rows = a.i32(8);
+  const int n_max = a.integer(9), advance = a.truth(10), lb = a.integer(11), le = a.integer(12);
+  RELEASED(dlm_kv_cache_commit_q4(ctx, cache, k, v, src_len, src_idx, dst_pos, dst_mode, n_rows, n_max, advance, lb, le, s));
+}
+
+const char* const kReadArgs[] = {"ctx", "cache", "src_pos", "n_rows", "n_max", "layer_begin", "layer_end", "k_out", "v_out"};
+int call_read_q4(Args& a) {
+  dlm_ctx* ctx = static_cast<dlm_ctx*>(a.handle(0));
+  const dlm_kv_cache_q4* cache = a.cache_q4(1);
+  const int32_t *src_pos = a.i32(2), *n_rows = a.i32(3);
+  const int n_max = a.integer(4), lb = a.integer(5), le = a.integer(6);
+  void *k = a.bf16(7), *v = a.bf16(8);
+  RELEASED(dlm_kv_cache_read_q4(ctx, cache, src_pos, n_rows, n_max, lb, le, k, v, s));
+}
+
+int call_attn_q4(Args& a) {
+  dlm_ctx* ctx = static_cast<dlm_ctx*>(a.handle(0));
+  const dlm_kv_cache_q4* cache = a.cache_q4(1);
+  const int lb = a.integer(2), le = a.integer(3);
+  const void *q = a.bf16(4), *k = a.bf16(5), *v = a.bf16(6);
+  const int heads = a.integer(7), q_cap = a.integer(8);
+  const int32_t* q_len = a.i32(9);
+  const float scale = a.real(10);
+  const int hint = a.integer(11);
+  void* out = a.bf16(12);
+  float* lse = a.f32(13);
+  size_t bytes;
+  void* ws = a.scratch(14, bytes);
+  RELEASED(dlm_freecache_attn_step_q4(ctx, cache, lb, le, q, k, v, heads, q_cap, q_len, scale, hint, out, lse, ws, bytes, s));
+}
+
+const char* const kWeightArgs[] = {"ctx", "cache", "layer_begin", "layer_end", "q", "lse", "n_q_heads", "q_cap", "q_len", "softmax_scale",
+                                   "cache_len_hint", "collected", "decay", "weight"};
+template <bool kQ4>
+int call_weight(Args& a) {
+  dlm_ctx* ctx = static_cast<dlm_ctx*>(a.handle(0));
+  const void* cache = kQ4 ? static_cast<const void*>(a.cache_q4(1)) : a.cache(1);
+  const int lb = a.integer(2), le = a.integer(3);
+  const void* q = a.bf16(4);
+  const float* lse = a.f32(5);
+  const int heads = a.integer(6), q_cap = a.integer(7);
+  const int32_t* q_len = a.i32(8);
+  const float scale = a.real(9);
+  const int hint = a.integer(10);
+  const float* collected = a.f32(11);
+  const float decay = a.real(12);
+  float* weight = a.f32(13);
+  RELEASED(kQ4 ? dlm_cache_weight_accumulate_q4(ctx, static_cast<const dlm_kv_cache_q4*>(cache), lb, le, q, lse, heads, q_cap, q_len, scale,
+                                                hint, collected, decay, weight, s)
+               : dlm_cache_weight_accumulate(ctx, static_cast<const dlm_kv_cache*>(cache), lb, le, q, lse, heads, q_cap, q_len, scale, hint,
+                                             collected, decay, weight, s));
+}
+
+const char* const kEvictArgs[] = {"ctx", "cache", "weight", "keep", "protect_first", "protect_last", "kept_idx", "weight_out"};
+template <bool kQ4>
+int call_evict(Args& a) {
+  dlm_ctx* ctx = static_cast<dlm_ctx*>(a.handle(0));
+  const void* cache = kQ4 ? static_cast<const void*>(a.cache_q4(1)) : a.cache(1);
+  const float* weight = a.f32(2);
+  const int keep = a.integer(3), first = a.integer(4), last = a.integer(5);
+  int32_t* kept = a.i32(6);
+  float* out = a.f32(7);
+  RELEASED(kQ4 ? dlm_kv_cache_evict_q4(ctx, static_cast<const dlm_kv_cache_q4*>(cache), weight, keep, first, last, kept, out, s)
+               : dlm_kv_cache_evict(ctx, static_cast<const dlm_kv_cache*>(cache), weight, keep, first, last, kept, out, s));
+}
+
 #define ENTRY(name, names, fn) {name, (int)(sizeof(names) / sizeof(names[0])), names, fn}
 const Entry kEntries[] = {
     ENTRY("dlm_kv_cache_commit", kCommitArgs, call_commit),
@@ -326,6 +400,13 @@ const Entry kEntries[] = {
     ENTRY("dlm_window_qkv_project_rope", kRopeArgs, call_rope),
     ENTRY("dlm_window_qkv_project_stage", kStageArgs, call_stage),
     ENTRY("dlm_window_out_project", kOutArgs, call_out),
+    ENTRY("dlm_kv_cache_commit_q4", kCommitArgs, call_commit_q4),
+    ENTRY("dlm_kv_cache_read_q4", kReadArgs, call_read_q4),
+    ENTRY("dlm_freecache_attn_step_q4", kAttnArgs, call_attn_q4),
+    ENTRY("dlm_cache_weight_accumulate", kWeightArgs, call_weight<false>),
+    ENTRY("dlm_cache_weight_accumulate_q4", kWeightArgs, call_weight<true>),
+    ENTRY("dlm_kv_cache_evict", kEvictArgs, call_evict<false>),
+    ENTRY("dlm_kv_cache_evict_q4", kEvictArgs, call_evict<true>),
 };
 constexpr int kNumEntries = sizeof(kEntries) / sizeof(kEntries[0]);
 constexpr int kMaxArgs = 24;
@@ -385,12 +466,14 @@ PyObject* set_error(PyObject*, PyObject* cls) {
 }
 
 PyObject* set_types(PyObject*, PyObject* args) {
-  PyObject *handle, *cache;
-  if (!PyArg_ParseTuple(args, "O!O!", &PyType_Type, &handle, &PyType_Type, &cache)) return nullptr;
+  PyObject *handle, *cache, *cache_q4;
+  if (!PyArg_ParseTuple(args, "O!O!O!", &PyType_Type, &handle, &PyType_Type, &cache, &PyType_Type, &cache_q4)) return nullptr;
   Py_INCREF(handle);
   Py_INCREF(cache);
+  Py_INCREF(cache_q4);
   Py_XSETREF(g_handle_type, reinterpret_cast<PyTypeObject*>(handle));
   Py_XSETREF(g_cache_type, reinterpret_cast<PyTypeObject*>(cache));
+  Py_XSETREF(g_cache_q4_type, reinterpret_cast<PyTypeObject*>(cache_q4));
   Py_RETURN_NONE;
 }
 

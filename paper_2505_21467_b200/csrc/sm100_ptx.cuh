@@ -175,6 +175,12 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst_smem, const void* tmap,
       : "memory");
 }
 
+// Untiled copy of `bytes` (a multiple of 16; both addresses on 16 bytes) into this block's shared memory.
+__device__ __forceinline__ void bulk_load(uint32_t dst_smem, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst_smem), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+
 // 4-d and 5-d tiled loads.  PAIR: the copy lands in this block's shared memory and completes on `bar`, a barrier of the
 // CTA pair's leader given as a shared::cluster address (map_shared_rank); otherwise `bar` is this block's own.
 template <bool PAIR>
