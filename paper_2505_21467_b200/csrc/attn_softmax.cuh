@@ -22,6 +22,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 // and the fp32 accumulators hold just as well; the final division by the row sum, taken against
 // the same maximum, cancels it.  Ragged half-steps compare maxima (kRescaleThreshold, log2 units);
 // full ones look at the row sum (kSumLimit).
+// (real = false: nobody reads the thread's row, which may hold anything; it does not take the warp through a rescaling.)
 constexpr float kRescaleThreshold = 8.0f;
 
 // Rare path shared by both kinds of half-step: some row of the warp outgrew its maximum by more
@@ -99,7 +100,7 @@ __device__ __forceinline__ float exp64_store(const uint32_t (&s)[64], float scal
 template <int D>
 __device__ __forceinline__ bool softmax_half_full(uint32_t t_s, uint32_t t_o, bool first, float scale_log2,
                                                   float& m_used, float& l_run, uint32_t bar_pv_done,
-                                                  uint32_t pv_parity, volatile int* abort_ptr) {
+                                                  uint32_t pv_parity, volatile int* abort_ptr, bool real = true) {
   uint32_t s[64];
   tmem_ld32(t_s, s);
   tmem_ld32(t_s + 32, s + 32);
@@ -110,7 +111,7 @@ __device__ __forceinline__ bool softmax_half_full(uint32_t t_s, uint32_t t_o, bo
   }
   float l_half = exp64_store(s, scale_log2, m_used, t_s);
   if (!first) {
-    const bool grow = !(l_half <= kSumLimit);   // also catches a NaN sum
+    const bool grow = real && !(l_half <= kSumLimit);   // also catches a NaN sum
     if (__any_sync(0xffffffffu, grow)) {
       const float m_new = row_max64<D>(s) * scale_log2;
       tmem_st_wait();   // the P just written is replaced below
@@ -128,7 +129,7 @@ __device__ __forceinline__ bool softmax_half_full(uint32_t t_s, uint32_t t_o, bo
 template <int D>
 __device__ __noinline__ bool softmax_half_ragged(uint32_t t_s, uint32_t t_o, int valid, bool first, float scale_log2,
                                                  float& m_used, float& l_run, uint32_t bar_pv_done,
-                                                 uint32_t pv_parity, volatile int* abort_ptr) {
+                                                 uint32_t pv_parity, volatile int* abort_ptr, bool real = true) {
   const int n_chunks = (valid + 31) >> 5;
   uint32_t v[32];
   float mx = -CUDART_INF_F;
@@ -144,7 +145,7 @@ __device__ __noinline__ bool softmax_half_ragged(uint32_t t_s, uint32_t t_o, int
     m_used = m_new;
     l_run = 0.f;
   } else {
-    const bool grow = m_new > m_used + kRescaleThreshold;
+    const bool grow = real && m_new > m_used + kRescaleThreshold;
     if (__any_sync(0xffffffffu, grow)) {
       if (!rescale_o<D>(t_o, grow, m_new, m_used, l_run, bar_pv_done, pv_parity, abort_ptr)) return false;
     }

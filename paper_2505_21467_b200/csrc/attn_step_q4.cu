@@ -8,8 +8,8 @@
 // then the fresh ones.  Block = 16 warps:
 //   warps 0-3    softmax of M tile 0 (128 query rows; thread = row = TMEM lane)
 //   warps 4-7    softmax of M tile 1, or with one M tile decoders like 8-11
-//   warps 8-11   decoders: packed K and V steps to bf16 operand tiles, a group of 32 values a thread at a time; one of their lanes
-//                has fresh rows copied straight into operand tiles (TMA)
+//   warps 8-11   decoders: packed K and V steps to bf16 operand tiles, a group of 32 values a thread at a time; two of their lanes
+//                have fresh rows copied straight into operand tiles (TMA)
 //   warp  12     producer (one lane): bulk copies of packed steps (a step's rows lie one after the other), TMA of Q
 //   warps 13, 14 tcgen05.mma issuers of M tile 0 / 1 (one lane each)
 // A step costs the tensor pipe about 1000 cycles with two M tiles, the softmax as much and the decoders 300 of each scheduler's issue
@@ -52,6 +52,7 @@ struct Shape {
   static constexpr int KS = NMT == 2 ? 4 : 3, VS = 3;        // operand tiles
   static constexpr int PS = NMT == 2 ? 4 : 8;                // packed steps in flight: with one M tile HBM is the bound
   static constexpr int kDecodeWarps = NMT == 2 ? 4 : 8;
+  static constexpr int kTeamWarps = kDecodeWarps / 4;        // of the teams K even, K odd, V even, V odd
   static constexpr int kTiles = NMT * kQTile + (KS + VS) * kTile + PS * kPackedStage;
   static constexpr uint32_t kColO = 0, kColS = 2 * D;        // O[mt] at mt * D, S[mt] at 2 D + mt * 128 (P in its place)
 };
@@ -172,18 +173,18 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       }
     }
     for (int i = 0; i < KS; ++i) {
-      mbar_init(bar_k_full + 8 * i, G::kDecodeWarps);
+      mbar_init(bar_k_full + 8 * i, 2 * G::kTeamWarps);
       mbar_init(bar_k_empty + 8 * i, NMT);
       mbar_init(bar_kf + 8 * i, 1);
     }
     for (int i = 0; i < VS; ++i) {
-      mbar_init(bar_v_full + 8 * i, G::kDecodeWarps);
+      mbar_init(bar_v_full + 8 * i, 2 * G::kTeamWarps);
       mbar_init(bar_v_empty + 8 * i, NMT);
       mbar_init(bar_vf + 8 * i, 1);
     }
     for (int i = 0; i < PS; ++i) {
       mbar_init(bar_p_full + 8 * i, 1);
-      mbar_init(bar_p_empty + 8 * i, G::kDecodeWarps);
+      mbar_init(bar_p_empty + 8 * i, 2 * G::kTeamWarps);
     }
     mbar_fence_init();
     fence_proxy_async_smem();
@@ -315,95 +316,93 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     }
   } else if (warp >= 8 || (NMT == 1 && warp >= 4)) {
     // ================================================================= decoders
+    // Four teams: K or V tiles, of the even or of the odd packed steps.  A tile costs a warp a chain of waits, loads, conversions, stores, a
+    // fence and an arrival, most of it latency: with all warps on the same tile, K then V, a step took 1900 cycles; so the chains of
+    // two steps and of K and V run beside each other.  Every team waits for every stage of its kind to be free and arrives for it, also where it has
+    // nothing to store, so that its arrivals cannot run ahead into the stage's next phase.
     setmaxnreg_dec<kRegsDecode>();
-    constexpr int kDecoders = G::kDecodeWarps * 32, kTasks = kStep * (D / q4::kGroup), kPer = (kTasks + kDecoders - 1) / kDecoders;
-    const int me = tid - (kThreads - 128 - kDecoders);
+    static_assert(PS % 2 == 0, "a packed stage belongs to one pair of teams");
+    constexpr int kThreadsOfTeam = G::kTeamWarps * 32, kTasks = kStep * (D / q4::kGroup), kPer = kTasks / kThreadsOfTeam, kBatch = 2;
+    const int w = warp - (kThreads / 32 - 4 - G::kDecodeWarps), team = w / G::kTeamWarps, me = tid & (kThreadsOfTeam - 1);
+    const bool is_k = team < 2, asks = (team & 1) == 0 && me == 0;
+    const uint32_t odd = team & 1, stages = is_k ? KS : VS, tiles = is_k ? sm_k : sm_v, part = is_k ? 0 : Pk::kBytes;
+    const uint32_t bar_full = is_k ? bar_k_full : bar_v_full, bar_empty = is_k ? bar_k_empty : bar_v_empty, bar_fresh = is_k ? bar_kf : bar_vf;
     auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_warp(bar, parity, abort_ptr, kLimit); };
-    // what was stored to a tile is visible to the tensor cores before the tile is announced
-    auto announce = [&](uint32_t bar) {
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar);
-    };
     Walk walk(p, len, deal, blockIdx.x);
     Segment g = {};
-    uint32_t st = 0, ps = 0, fs = 0, fk = 0, fv = 0;   // steps, packed and fresh ones so far; fresh K and V tiles asked for (by one lane)
+    uint32_t st = 0, ps = 0, fs = 0, asked = 0;   // steps, packed and fresh ones so far; fresh tiles asked for (by one lane)
     bool ok = true;
     while (ok && walk.next(g)) {
-      int t_k = max(g.n_c, g.begin), t_v = t_k;   // the fresh steps whose K and V are asked for next
+      int t_ask = max(g.n_c, g.begin);   // the fresh step whose tile is asked for next
       for (int t = g.begin; t < g.end && ok; ++t, ++st) {
-        // One lane of the decoders copies the fresh rows, as far ahead as there are operand tiles free.  (Not the producer: it runs further
-        // ahead of the products than a stage's barrier can tell, since a wait for a phase works only when the one before it is over.)
-        if (me == 0 && ((t_k < g.end && t_k - t < KS) || (t_v < g.end && t_v - t < VS))) {
-          const int z = (g.layer * p.batch + g.b) * p.n_kv_heads + g.kvh;
-          const uint32_t bytes = (uint32_t)p.fresh_box * 128u * G::kPanels;
-          // the stage is free: for the step at hand wait for that, for later ones only look
-          auto free_stage = [&](uint32_t bar, uint32_t use, bool now) {
-            if (use == 0) return true;
-            return now ? mbar_wait_limit(bar, (use - 1) & 1, abort_ptr, kLimit) : mbar_test_wait(bar, (use - 1) & 1);
-          };
-          for (; t_k < g.end && t_k - t < KS; ++t_k, ++fk) {
-            const uint32_t i = st + (t_k - t), s = i % KS, bar = bar_kf + 8 * (fk % KS);
-            if (!free_stage(bar_k_empty + 8 * s, i / KS, t_k == t)) break;
-            mbar_expect_tx(bar, bytes);
-            for (int pn = 0; pn < G::kPanels; ++pn) tma_load_3d(sm_k + s * G::kTile + pn * G::kPanel, &tm_kn, bar, pn * 64, (t_k - g.n_c) * kStep, z);
-          }
-          for (; t_v < g.end && t_v - t < VS; ++t_v, ++fv) {
-            const uint32_t i = st + (t_v - t), s = i % VS, bar = bar_vf + 8 * (fv % VS);
-            if (!free_stage(bar_v_empty + 8 * s, i / VS, t_v == t)) break;
-            mbar_expect_tx(bar, bytes);
-            for (int pn = 0; pn < G::kPanels; ++pn) tma_load_3d(sm_v + s * G::kTile + pn * G::kPanel, &tm_vn, bar, pn * 64, (t_v - g.n_c) * kStep, z);
+        // One lane of the K teams and one of the V teams copy the fresh rows, as far ahead as there are tiles free: for the step at hand they
+        // wait for that, for later ones they only look.  (Not the producer: it runs further ahead of the products than a
+        // stage's barrier can tell, since a wait for a phase works only when the one before it is over.)
+        if (asks) {
+          for (; t_ask < g.end && t_ask - t < (int)stages; ++t_ask, ++asked) {
+            const uint32_t i = st + (t_ask - t), s = i % stages, bar = bar_fresh + 8 * (asked % stages), parity = (i / stages - 1) & 1;
+            if (i >= stages && !(t_ask == t ? mbar_wait_limit(bar_empty + 8 * s, parity, abort_ptr, kLimit) : mbar_test_wait(bar_empty + 8 * s, parity))) break;
+            mbar_expect_tx(bar, (uint32_t)p.fresh_box * 128u * G::kPanels);
+            for (int pn = 0; pn < G::kPanels; ++pn)
+              tma_load_3d(tiles + s * G::kTile + pn * G::kPanel, is_k ? &tm_kn : &tm_vn, bar, pn * 64, (t_ask - g.n_c) * kStep,
+                          (g.layer * p.batch + g.b) * p.n_kv_heads + g.kvh);
           }
         }
         __syncwarp();
-        const uint32_t ks = st % KS, vs = st % VS;
-        const uint32_t k_tile = sm_k + ks * G::kTile, v_tile = sm_v + vs * G::kTile;
+        const uint32_t stage = st % stages, tile = tiles + stage * G::kTile;
         const int keys = step_keys(g, t), n16 = (keys + 15) & ~15;
-        if (t < g.n_c) {
-          const uint32_t s = ps % PS, packed = sm_p + s * G::kPackedStage;
-          ok = wait(bar_p_full + 8 * s, (ps / PS) & 1);
+        // V rows from `keys` to the next multiple of 16 meet P = 0: clear them, so that a NaN left there cannot reach O
+        auto clear_rest = [&]() {
+          if (!is_k)
+            for (int i = keys * (D / 8) + me; i < n16 * (D / 8); i += kThreadsOfTeam) q4::clear_piece<D>(tile, G::kPanel, i);
+        };
+        const bool fresh = t >= g.n_c, mine = !fresh && (ps++ & 1) == odd;
+        if (!mine && st >= stages) {
+          ok = wait(bar_empty + 8 * stage, (st / stages - 1) & 1);
           if (!ok) break;
-          q4::Group32 kg[kPer], vg[kPer];
+        }
+        if (fresh) {
+          ok = wait(bar_fresh + 8 * (fs % stages), (fs / stages) & 1);
+          if (!ok) break;
+          ++fs;
+          if (odd == 0) clear_rest();
+        } else if (mine) {
+          const uint32_t s = (ps - 1) % PS, packed = sm_p + s * G::kPackedStage + part;
+          ok = wait(bar_p_full + 8 * s, ((ps - 1) / PS) & 1);
+          if (!ok) break;
+          if (st >= stages) {
+            ok = wait(bar_empty + 8 * stage, (st / stages - 1) & 1);
+            if (!ok) break;
+          }
+          // (a short loop: unrolled, this code and the softmax's drive each other out of the instruction caches)
           const int tasks = keys * (D / q4::kGroup);
+#pragma unroll 1
+          for (int i0 = 0; i0 < kPer; i0 += kBatch) {
+            q4::Group32 x[kBatch];
 #pragma unroll
-          for (int i = 0; i < kPer; ++i) {
-            const int task = me + i * kDecoders;
-            if (task < tasks) {
-              kg[i] = q4::read_group<D>(packed, task);
-              vg[i] = q4::read_group<D>(packed + Pk::kBytes, task);
+            for (int i = 0; i < kBatch; ++i) {
+              const int task = me + (i0 + i) * kThreadsOfTeam;
+              if (task < tasks) x[i] = q4::read_group<D>(packed, task);
+            }
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+              const int task = me + (i0 + i) * kThreadsOfTeam;
+              if (task < tasks) q4::write_group<D>(tile, G::kPanel, task, x[i]);
             }
           }
           __syncwarp();
           if (lane == 0) mbar_arrive(bar_p_empty + 8 * s);
-          ++ps;
-          if (st >= (uint32_t)KS) ok = wait(bar_k_empty + 8 * ks, (st / KS - 1) & 1);
-          if (!ok) break;
-#pragma unroll
-          for (int i = 0; i < kPer; ++i)
-            if (me + i * kDecoders < tasks) q4::write_group<D>(k_tile, G::kPanel, me + i * kDecoders, kg[i]);
-          announce(bar_k_full + 8 * ks);
-          if (st >= (uint32_t)VS) ok = wait(bar_v_empty + 8 * vs, (st / VS - 1) & 1);
-          if (!ok) break;
-#pragma unroll
-          for (int i = 0; i < kPer; ++i)
-            if (me + i * kDecoders < tasks) q4::write_group<D>(v_tile, G::kPanel, me + i * kDecoders, vg[i]);
-        } else {
-          ok = wait(bar_kf + 8 * (fs % KS), (fs / KS) & 1);
-          if (!ok) break;
-          announce(bar_k_full + 8 * ks);
-          ok = wait(bar_vf + 8 * (fs % VS), (fs / VS) & 1);
-          if (!ok) break;
-          ++fs;
+          clear_rest();
         }
-        // V rows from `keys` to the next multiple of 16 meet P = 0: clear them, so that a NaN left there cannot reach O
-        for (int i = keys * (D / 8) + me; i < n16 * (D / 8); i += kDecoders) q4::clear_piece<D>(v_tile, G::kPanel, i);
-        announce(bar_v_full + 8 * vs);
+        // what was stored to the tile is visible to the tensor cores before it is announced
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_full + 8 * stage);
       }
     }
     // no copy lands after the block has released its shared memory (here and in the producer: they have landed long since unless the
     // block is unwinding)
-    for (uint32_t i = fk > (uint32_t)KS ? fk - KS : 0; i < fk; ++i) mbar_wait(bar_kf + 8 * (i % KS), (i / KS) & 1, never_ptr);
-    for (uint32_t i = fv > (uint32_t)VS ? fv - VS : 0; i < fv; ++i) mbar_wait(bar_vf + 8 * (i % VS), (i / VS) & 1, never_ptr);
+    for (uint32_t i = asked > stages ? asked - stages : 0; i < asked; ++i) mbar_wait(bar_fresh + 8 * (i % stages), (i / stages) & 1, never_ptr);
   } else {
     // ================================================================= softmax warps (those that own real rows)
     setmaxnreg_inc<kRegsSoftmax>();
@@ -434,6 +433,8 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       bool ok = true;
       while (ok && walk.next(g)) {
         float m_used = -CUDART_INF_F, l_run = 0.f;
+        const int r_kv = g.rc * p.chunk + r_unit;
+        const bool real = r_unit < p.rows && r_kv < p.rows_total, active = real && r_kv - p.by_q_cap.div(r_kv) * p.q_cap < g.Lq;
         for (int t = g.begin; t < g.end; ++t, ++st) {
           const uint32_t buf = st & 1, before = 16 * mt + 8 * ((st - 1) & 1), parity = ((st - 1) >> 1) & 1;
           ok = wait(bar_s_ready + 16 * mt + 8 * buf, (st >> 1) & 1);
@@ -441,9 +442,9 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           tc_fence_after_sync();
           const int keys = step_keys(g, t);
           if (keys == kStep)
-            ok = softmax_half_full<D>(t_s + buf * kStep, t_o, t == g.begin, p.scale_log2, m_used, l_run, bar_pv_done + before, parity, abort_ptr);
+            ok = softmax_half_full<D>(t_s + buf * kStep, t_o, t == g.begin, p.scale_log2, m_used, l_run, bar_pv_done + before, parity, abort_ptr, active);
           else
-            ok = softmax_half_ragged<D>(t_s + buf * kStep, t_o, keys, t == g.begin, p.scale_log2, m_used, l_run, bar_pv_done + before, parity, abort_ptr);
+            ok = softmax_half_ragged<D>(t_s + buf * kStep, t_o, keys, t == g.begin, p.scale_log2, m_used, l_run, bar_pv_done + before, parity, abort_ptr, active);
           if (!ok) break;
           __syncwarp();
           if (lane == 0) {
@@ -455,11 +456,8 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         if (ok) ok = wait(bar_pv_done + 16 * mt + 8 * ((st - 1) & 1), ((st - 1) >> 1) & 1);
         if (!ok) break;
         tc_fence_after_sync();
-        const int r_kv = g.rc * p.chunk + r_unit;
-        const bool real = r_unit < p.rows && r_kv < p.rows_total;
         uint32_t v[32];
         if (g.slot < 0) {
-          const bool active = real && r_kv - p.by_q_cap.div(r_kv) * p.q_cap < g.Lq;
           const float inv = active ? 1.f / l_run : 0.f;
           const size_t r = out_row(g.layer, g.b, g.kvh, g.rc);
 #pragma unroll 1

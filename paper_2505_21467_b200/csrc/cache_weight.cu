@@ -128,7 +128,7 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   if (tid == 0) {
     *abort_ptr = 0; *never_ptr = 0;
     for (int i = 0; i < KS; ++i) {
-      mbar_init(bar_k_full + 8 * i, kQ4 ? kDecodeWarps : 1);
+      mbar_init(bar_k_full + 8 * i, kQ4 ? kDecodeWarps / 2 : 1);
       mbar_init(bar_k_empty + 8 * i, 1);
     }
     for (int i = 0; i < PS; ++i) {
@@ -311,33 +311,46 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     }
   } else if (warp >= 8) {
     if (kQ4) {
-      // ================================================================= decoders
-      constexpr int kGroups = D / q4::kGroup, kPer = kKeys * kGroups / (kDecodeWarps * 32);
-      const int me = tid - 256;
-      uint32_t kt = 0, tiles[2] = {0, 0};
+      // ================================================================= decoders: two warps for either group's tiles
+      constexpr int kGroups = D / q4::kGroup, kPer = kKeys * kGroups / 64, kBatch = 4;
+      const int me = tid & 63, w = (warp - 8) >> 1;
+      uint32_t kt = 0, n = 0;   // tiles, the group's tiles
       while (ok && walk.next(g)) {
         for (int t = g.begin; t < g.end && ok; ++t, ++kt) {
-          const int w = (t - g.begin) & 1;
-          const uint32_t n = w ? tiles[1]++ : tiles[0]++;
-          const uint32_t s = kt % PS, ks = 2 * w + (n & 1), packed = sm_p + s * G::kPackedStage, tile = sm_k + ks * G::kTile;
+          const uint32_t s = kt % PS, packed = sm_p + s * G::kPackedStage;
           ok = mbar_wait_warp(bar_p_full + 8 * s, (kt / PS) & 1, abort_ptr);
           if (!ok) break;
+          if (((t - g.begin) & 1) != w) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_p_empty + 8 * s);
+            continue;
+          }
+          const uint32_t ks = 2 * w + (n & 1), tile = sm_k + ks * G::kTile;
           const int tasks = min(kKeys, g.Lc - t * kKeys) * kGroups;
-          q4::Group32 x[kPer];
 #pragma unroll
-          for (int i = 0; i < kPer; ++i) {
-            const int task = me + i * kDecodeWarps * 32, half = task / (64 * kGroups);
-            if (task < tasks) x[i] = q4::read_group<D>(packed + half * Pk::kBytes, task - half * 64 * kGroups);
+          for (int i0 = 0; i0 < kPer; i0 += kBatch) {
+            q4::Group32 x[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+              const int task = me + (i0 + i) * 64, half = task / (64 * kGroups);
+              if (task < tasks) x[i] = q4::read_group<D>(packed + half * Pk::kBytes, task - half * 64 * kGroups);
+            }
+            if (i0 + kBatch == kPer) {
+              __syncwarp();
+              if (lane == 0) mbar_arrive(bar_p_empty + 8 * s);
+            }
+            if (i0 == 0 && n >= 2) {
+              ok = mbar_wait_warp(bar_k_empty + 8 * ks, ((n >> 1) - 1) & 1, abort_ptr);
+              if (!ok) break;
+            }
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+              const int task = me + (i0 + i) * 64;
+              if (task < tasks) q4::write_group<D>(tile, G::kPanel, task, x[i]);
+            }
           }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar_p_empty + 8 * s);
-          if (n >= 2) ok = mbar_wait_warp(bar_k_empty + 8 * ks, ((n >> 1) - 1) & 1, abort_ptr);
           if (!ok) break;
-#pragma unroll
-          for (int i = 0; i < kPer; ++i) {
-            const int task = me + i * kDecodeWarps * 32;
-            if (task < tasks) q4::write_group<D>(tile, G::kPanel, task, x[i]);
-          }
+          ++n;
           fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) mbar_arrive(bar_k_full + 8 * ks);
