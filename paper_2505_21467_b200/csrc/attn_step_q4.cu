@@ -48,7 +48,7 @@ struct Shape {
   static constexpr int kQTile = kPanels * kQPanel;
   static constexpr int kPanel = kStep * 128;
   static constexpr int kTile = kPanels * kPanel;             // a step of K or V
-  static constexpr int kPackedStage = 2 * q4::Packed<D>::kBytes;
+  static constexpr int kPackedStage = 2 * q4::Packed<D, kStep>::kBytes;
   static constexpr int KS = NMT == 2 ? 4 : 3, VS = 3;        // operand tiles
   static constexpr int PS = NMT == 2 ? 4 : 8;                // packed steps in flight: with one M tile HBM is the bound
   static constexpr int kDecodeWarps = NMT == 2 ? 4 : 8;
@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_kn,
                     const __grid_constant__ CUtensorMap tm_vn, const __grid_constant__ Params p) {
   using G = Shape<D, NMT>;
-  using Pk = q4::Packed<D>;
+  using Pk = q4::Packed<D, kStep>;
   constexpr uint64_t kLimit = kNoWait ? 0ull : kWaitLimitNs;
   constexpr int KS = G::KS, VS = G::VS, PS = G::PS;
   extern __shared__ uint8_t smem_raw[];
@@ -209,7 +209,7 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 
   if (warp >= 12) {
     setmaxnreg_dec<kRegsControl>();
-    if (warp == 12 && lane == 0) {
+    if (warp == 12) {
       // ================================================================= producer
       Walk walk(p, len, deal, blockIdx.x);
       Segment g = {};
@@ -217,34 +217,36 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       bool ok = true, q_due = false;
       auto issue_q = [&]() {
         q_due = false;
-        if (n_q > 0 && !mbar_wait_limit(bar_q_empty, (n_q - 1) & 1, abort_ptr, kLimit)) return false;
-        const int z = (g.layer * p.batch + g.b) * p.n_kv_heads + g.kvh;
-        mbar_expect_tx(bar_q_full, (uint32_t)(NMT * min(128, p.rows)) * 128u * G::kPanels);   // a box counts in full
-        for (int mt = 0; mt < NMT; ++mt)
-          for (int pn = 0; pn < G::kPanels; ++pn)
-            tma_load_3d(sm_q + mt * G::kQTile + pn * G::kQPanel, &tm_q, bar_q_full, pn * 64, g.rc * p.chunk + mt * 128, z);
+        if (n_q > 0 && !mbar_wait_warp(bar_q_empty, (n_q - 1) & 1, abort_ptr, kLimit)) return false;
+        const int z = (g.layer * p.batch + g.b) * p.n_kv_heads + g.kvh, mt = lane / G::kPanels, pn = lane % G::kPanels;
+        if (lane == 0) mbar_expect_tx(bar_q_full, (uint32_t)(NMT * min(128, p.rows)) * 128u * G::kPanels);   // a box counts in full
+        __syncwarp();
+        if (mt < NMT) tma_load_3d(sm_q + mt * G::kQTile + pn * G::kQPanel, &tm_q, bar_q_full, pn * 64, g.rc * p.chunk + mt * 128, z);
+        __syncwarp();
         ++n_q;
         return true;
       };
-      // Q is copied as soon as the unit before has done with its own, and at the latest where this lane would wait for the
+      // Q is copied as soon as the unit before has done with its own, and at the latest where this warp would wait for the
       // steps that need it
       auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (q_due && ((n_q == 0 || mbar_test_wait(bar_q_empty, (n_q - 1) & 1)) || !mbar_test_wait(bar, parity)) && !issue_q()) return false;
-        return mbar_wait_limit(bar, parity, abort_ptr, kLimit);
+        if (q_due && (n_q == 0 || mbar_test_wait_warp(bar_q_empty, (n_q - 1) & 1) || !mbar_test_wait_warp(bar, parity)) && !issue_q()) return false;
+        return mbar_wait_warp(bar, parity, abort_ptr, kLimit);
       };
       while (ok && walk.next(g)) {
         q_due = true;
         if (n_q == 0) ok = issue_q();
         const size_t head = ((size_t)(g.layer + p.layer_begin) * p.batch + g.b) * p.n_kv_heads + g.kvh;
         for (int t = g.begin; t < min(g.end, g.n_c) && ok; ++t, ++ps) {
-          const uint32_t s = ps % PS, dst = sm_p + s * G::kPackedStage, bar = bar_p_full + 8 * s;
+          const uint32_t s = ps % PS, bar = bar_p_full + 8 * s;
           if (ps >= (uint32_t)PS) ok = wait(bar_p_empty + 8 * s, (ps / PS - 1) & 1);
           if (!ok) break;
           const int rows = step_keys(g, t);
-          const size_t row = head * p.capacity + (size_t)t * kStep;
-          mbar_expect_tx(bar, 2 * Pk::bytes(rows));
-          Pk::copy(dst, p.k, p.k_scale, row, rows, bar);
-          Pk::copy(dst + Pk::kBytes, p.v, p.v_scale, row, rows, bar);
+          if (lane == 0) mbar_expect_tx(bar, 2 * Pk::bytes(rows));
+          __syncwarp();
+          if (lane < 4)   // values and scales of K and of V
+            Pk::copy_part(sm_p + s * G::kPackedStage + (lane >> 1) * Pk::kBytes, lane < 2 ? p.k : p.v, lane < 2 ? p.k_scale : p.v_scale, lane & 1,
+                          head * p.capacity + (size_t)t * kStep, rows, bar);
+          __syncwarp();
         }
         if (ok && q_due) ok = issue_q();
       }
@@ -382,7 +384,7 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 #pragma unroll
             for (int i = 0; i < kBatch; ++i) {
               const int task = me + (i0 + i) * kThreadsOfTeam;
-              if (task < tasks) x[i] = q4::read_group<D>(packed, task);
+              if (task < tasks) x[i] = q4::read_group<D, kStep>(packed, task);
             }
 #pragma unroll
             for (int i = 0; i < kBatch; ++i) {
@@ -529,31 +531,35 @@ __global__ void __launch_bounds__(D * 4) q4_attention_join_kernel(const __grid_c
   if (row >= p.rows || r_kv >= p.rows_total) return;
   const bool active = r_kv - p.by_q_cap.div(r_kv) * p.q_cap < g.Lq;
   const size_t out = (((size_t)g.layer * p.batch + g.b) * p.n_q_heads + (size_t)g.kvh * p.group) * p.q_cap + r_kv;
-  // the part of block b: its first segment if the part starts where its share does, else its second
-  auto slot = [&](int b) { return (size_t)(d.lo(b) >= g.unit_begin ? 2 * b : 2 * b + 1); };
+  // the part of block b: its first segment if the part starts where its share does, as all but the first part do, else its second
+  const int first_slot = 2 * c_first + (d.lo(c_first) >= g.unit_begin ? 0 : 1);
+  constexpr int kAtOnce = 6;
   float m = -CUDART_INF_F, l = 0.f, o[8] = {};
-  for (int b0 = c_first; b0 <= c_last; b0 += 4) {
-    float2 ml[4];
-    float4 x[4], y[4];
+#pragma unroll 1
+  for (int b0 = c_first; b0 <= c_last; b0 += kAtOnce) {
+    float2 ml[kAtOnce];
+    float4 x[kAtOnce], y[kAtOnce];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < kAtOnce; ++j) {
       ml[j] = make_float2(-CUDART_INF_F, 0.f);
       x[j] = y[j] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (b0 + j <= c_last) {
-        const size_t s = slot(b0 + j);
+        const size_t s = (size_t)(b0 + j == c_first ? first_slot : 2 * (b0 + j));
         const float4* po = p.ws_o + (s * (D / 4) + 2 * c8) * p.rows_pad + row;
         ml[j] = __ldcg(p.ws_ml + s * p.rows_pad + row);
         x[j] = __ldcg(po);
         y[j] = __ldcg(po + p.rows_pad);
       }
     }
-    const float m_new = fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), m);
+    float m_new = m;
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) m_new = fmaxf(m_new, ml[j].x);
     const float old = ex2_approx(m - m_new);   // the first time 2^-inf = 0
     l *= old;
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] *= old;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < kAtOnce; ++j) {
       const float w = ex2_approx(ml[j].x - m_new);
       l = fmaf(w, ml[j].y, l);
       o[0] = fmaf(w, x[j].x, o[0]); o[1] = fmaf(w, x[j].y, o[1]); o[2] = fmaf(w, x[j].z, o[2]); o[3] = fmaf(w, x[j].w, o[3]);

@@ -7,12 +7,14 @@
 // no atomics.  Per (key, query) the tensor pipe needs 2 D flops and the thread one fused multiply-add, an exponential and an addition.
 //
 // A step is a tile of 128 keys of a (layer, batch element, KV head) against 128 query rows; a tile meets all query rows of its KV head.
-// Block = 16 warps, one block per SM with a contiguous share of the tiles:
-//   warps 0-3, 4-7   sums of every other tile (two score buffers of 128 columns each)
-//   warps 8-11       4-bit cache: decoders of K tiles
-//   warp  12         producer (one lane): K tiles by TMA (bf16) or bulk copies (4 bits), query rows by TMA
-//   warps 13, 14     tcgen05.mma issuers for warps 0-3 / 4-7 (one lane each)
-//   warp  15         the query rows' logarithms, and zeros for query rows that take no part
+// Block = 28 warps (20 without decoders), one block per SM with a contiguous share of the tiles:
+//   warps 0-15       sums of every other tile (two score buffers of 128 columns each), the first or second half of a step's columns: a warp's
+//                    chain of loads, multiply-adds, exponentials and additions is all latency, so four chains run beside each
+//                    other on each scheduler (28 layers at 16301 rows, bf16: 181 us with two)
+//   8 more           4-bit cache: decoders of K tiles, four warps for either group's
+//   then             producer (one lane): K tiles by TMA (bf16) or bulk copies (4 bits), query rows by TMA
+//   two              tcgen05.mma issuers for the two groups (one lane each)
+//   the last         the query rows' logarithms, and zeros for query rows that take no part
 // Query rows lie in two slots of 128: up to 256 stay there for all tiles of a unit, more go through for every pair of tiles.
 #include <cuda_bf16.h>
 #include <math_constants.h>
@@ -26,7 +28,6 @@ namespace {
 
 using namespace sm100;
 
-constexpr int kThreads = 512;
 constexpr int kKeys = 128;                // a tile
 constexpr int kRows = 128;                // query rows of a step
 constexpr int kMaxBatch = 1024;
@@ -34,19 +35,20 @@ constexpr int kMaxQCap = 4096;
 constexpr int kMaxGrid = 256;
 constexpr int kTmemCols = 512;
 constexpr int kBarrierBytes = 512, kFlagBytes = 64;
-constexpr int kDecodeWarps = 4;
+constexpr int kSumWarps = 16;             // two halves of the columns for either group of tiles
 
-template <int D>
+template <int D, bool kQ4>
 struct Shape {
+  static constexpr int kDecodeWarps = kQ4 ? 8 : 0, kThreads = 32 * (kSumWarps + kDecodeWarps + 4);
   static constexpr int kPanels = D / 64;
-  static constexpr int kPanel = 128 * 128;           // bytes: 128 rows of 64 values, K tile and query slot alike
+  static constexpr int kPanel = 128 * 128;           // bytes of a K tile's panel: 128 rows of 64 values
   static constexpr int kTile = kPanels * kPanel;
   static constexpr int KS = 4;                       // K tiles, two for either group of warps
-  static constexpr int PS = 3;                       // packed K tiles
-  static constexpr int kPackedStage = 2 * q4::Packed<D>::kBytes;   // two runs of 64 rows
-  static constexpr int kLogBytes = 2 * kRows * 4;
-  static constexpr int kTiles = (2 + KS) * kTile;
+  static constexpr int kPackedStage = q4::Packed<D, kKeys>::kBytes;
 };
+constexpr int kMaxPacked = 8;                        // packed K tiles: as many as there is room for
+constexpr int kLogBytes = 2 * kRows * 4;
+constexpr int kPartBytes = 2 * 4 * kKeys * 4;        // the second half's sums of a group's last four tiles
 
 struct Params {
   const int32_t* cache_len;
@@ -59,6 +61,8 @@ struct Params {
   int nl, layer_begin, batch, n_kv_heads, n_q_heads, group, capacity, q_cap;
   int rows_total, n_qc;         // query rows of a KV head, chunks of 128 of them
   int q_box, k_box;             // rows of the TMA boxes
+  uint32_t q_panel;             // bytes of a query slot's panel: as many rows as a chunk has, in whole groups of 16
+  int n_packed;                 // packed stages
   FastDiv by_kv_heads, by_q_cap;
   float scale_log2;
   int* status;
@@ -94,6 +98,16 @@ struct Walk {
   }
 };
 
+struct Ring {   // the next use of a ring of n stages: which stage, and the parity of its barrier's phase
+  uint32_t stage = 0, parity = 0;
+  __device__ __forceinline__ void advance(uint32_t n) {
+    if (++stage == n) {
+      stage = 0;
+      parity ^= 1u;
+    }
+  }
+};
+
 // Tiles begin, begin + 2, .. of a segment belong to group 0 of the warps, the others to group 1; tile i of a group (counted over the block's
 // life) has K stage 2 * group + (i & 1).  Every role enumerates the loads of query rows alike: events, event e in slot e & 1.  Up to two chunks:
 // one event each for a segment; more: one each for a pair of tiles.
@@ -102,57 +116,59 @@ struct Walk {
 // phase or waits behind something that does: hence stages that belong to one group, and events that each role takes, also where it has
 // no tile.
 template <int D, bool kQ4>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Shape<D, kQ4>::kThreads, 1)
 cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ Params p) {
-  using G = Shape<D>;
-  using Pk = q4::Packed<D>;
-  constexpr int KS = G::KS, PS = G::PS;
+  using G = Shape<D, kQ4>;
+  using Pk = q4::Packed<D, kKeys>;
+  constexpr int KS = G::KS, kControl = kSumWarps + G::kDecodeWarps;
+  const uint32_t PS = (uint32_t)p.n_packed, q_slot = G::kPanels * p.q_panel;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_pad = (1024u - (smem_u32(smem_raw) & 1023u)) & 1023u;
-  const uint32_t sm_q = smem_u32(smem_raw) + smem_pad, sm_k = sm_q + 2 * G::kTile, sm_p = sm_k + KS * G::kTile;
-  const uint32_t packed_bytes = kQ4 ? PS * G::kPackedStage : 0;
-  const uint32_t sm_log = sm_p + packed_bytes, sm_bar = sm_log + G::kLogBytes;
-  int* const flags = reinterpret_cast<int*>(smem_raw + smem_pad + G::kTiles + packed_bytes + G::kLogBytes + kBarrierBytes);
-  float* const logs = reinterpret_cast<float*>(smem_raw + smem_pad + G::kTiles + packed_bytes);
+  const uint32_t sm_k = smem_u32(smem_raw) + smem_pad, sm_q = sm_k + KS * G::kTile, sm_p = sm_q + 2 * q_slot;
+  const uint32_t sm_log = sm_p + (kQ4 ? PS * G::kPackedStage : 0), sm_part = sm_log + kLogBytes, sm_bar = sm_part + kPartBytes;
+  float* const logs = reinterpret_cast<float*>(smem_raw + smem_pad + (sm_log - sm_k));
+  float* const parts = reinterpret_cast<float*>(smem_raw + smem_pad + (sm_part - sm_k));   // [group][tile & 3][key]
+  int* const flags = reinterpret_cast<int*>(smem_raw + smem_pad + (sm_bar - sm_k) + kBarrierBytes);
   volatile int* const abort_ptr = flags;
   volatile int* const never_ptr = flags + 1;
   uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(flags + 2);
   const Lengths len(flags + kFlagBytes / 4, p.batch);
 
-  const uint32_t bar_k_full = sm_bar, bar_k_empty = bar_k_full + 8 * KS, bar_p_full = bar_k_empty + 8 * KS, bar_p_empty = bar_p_full + 8 * PS;
-  const uint32_t bar_q_tx = bar_p_empty + 8 * PS, bar_q_ready = bar_q_tx + 16, bar_q_empty = bar_q_ready + 16;   // [slot]
+  const uint32_t bar_k_full = sm_bar, bar_k_empty = bar_k_full + 8 * KS, bar_p_full = bar_k_empty + 8 * KS, bar_p_empty = bar_p_full + 8 * kMaxPacked;
+  const uint32_t bar_q_tx = bar_p_empty + 8 * kMaxPacked, bar_q_ready = bar_q_tx + 16, bar_q_empty = bar_q_ready + 16;   // [slot]
   const uint32_t bar_s_ready = bar_q_empty + 16, bar_s_empty = bar_s_ready + 32;                                // [warp group][buffer]
-  const uint32_t bar_drain = bar_s_empty + 32;                                                                 // [2]
+  const uint32_t bar_drain = bar_s_empty + 32, bar_part = bar_drain + 16;                                       // [2], [group][tile & 3]
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     *abort_ptr = 0; *never_ptr = 0;
     for (int i = 0; i < KS; ++i) {
-      mbar_init(bar_k_full + 8 * i, kQ4 ? kDecodeWarps / 2 : 1);
+      mbar_init(bar_k_full + 8 * i, kQ4 ? G::kDecodeWarps / 2 : 1);
       mbar_init(bar_k_empty + 8 * i, 1);
     }
-    for (int i = 0; i < PS; ++i) {
+    for (int i = 0; kQ4 && i < kMaxPacked; ++i) {
       mbar_init(bar_p_full + 8 * i, 1);
-      mbar_init(bar_p_empty + 8 * i, kDecodeWarps);
+      mbar_init(bar_p_empty + 8 * i, G::kDecodeWarps);
     }
+    for (int i = 0; i < 8; ++i) mbar_init(bar_part + 8 * i, 4);
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar_q_tx + 8 * i, 1);
       mbar_init(bar_q_ready + 8 * i, 1);
-      mbar_init(bar_q_empty + 8 * i, 10);    // the warps that sum, the issuers
+      mbar_init(bar_q_empty + 8 * i, kSumWarps + 2);   // and the issuers
       mbar_init(bar_drain + 8 * i, 1);
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(bar_s_ready + 8 * i, 1);
-      mbar_init(bar_s_empty + 8 * i, 4);
+      mbar_init(bar_s_empty + 8 * i, kSumWarps / 2);
     }
     mbar_fence_init();
     fence_proxy_async_smem();
   }
-  if (warp == 13) {
+  if (warp == kControl + 1) {
     tmem_alloc(smem_u32(tmem_slot), kTmemCols);
     tmem_relinquish();
   }
-  if (warp == 12 && lane == 0) {
+  if (warp == kControl && lane == 0) {
     prefetch_tensormap(&tm_q);
     if (!kQ4) prefetch_tensormap(&tm_k);
   }
@@ -171,63 +187,68 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   Segment g = {};
   bool ok = true;
 
-  if (warp == 12) {
-    if (lane == 0) {
-      // ================================================================= producer
-      uint32_t kt = 0, ev = 0, tiles[2] = {0, 0};   // packed tiles, events, tiles of the groups
-      auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait(bar, parity, abort_ptr); };
-      auto load_q = [&](int c) {
-        const uint32_t s = ev & 1;
-        if (ev >= 2 && !wait(bar_q_empty + 8 * s, ((ev >> 1) - 1) & 1)) return false;
+  if (warp == kControl) {
+    // ================================================================= producer
+    uint32_t kt = 0, ev = 0, tiles[2] = {0, 0};   // packed tiles, events, tiles of the groups
+    Ring ps;
+    auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_warp(bar, parity, abort_ptr); };
+    auto load_q = [&](int c) {
+      const uint32_t s = ev & 1;
+      if (ev >= 2 && !wait(bar_q_empty + 8 * s, ((ev >> 1) - 1) & 1)) return false;
+      if (lane == 0) {
         mbar_expect_tx(bar_q_tx + 8 * s, (uint32_t)p.q_box * 128u * G::kPanels);   // a box counts in full
         const int z = (g.layer * p.batch + g.b) * p.n_kv_heads + g.kvh;
-        for (int pn = 0; pn < G::kPanels; ++pn) tma_load_3d(sm_q + s * G::kTile + pn * G::kPanel, &tm_q, bar_q_tx + 8 * s, pn * 64, c * kRows, z);
-        ++ev;
-        return true;
-      };
-      auto load_k = [&](int t, int w) {
-        const int z = ((g.layer + p.layer_begin) * p.batch + g.b) * p.n_kv_heads + g.kvh;
-        if (kQ4) {
-          const uint32_t s = kt % PS, bar = bar_p_full + 8 * s, dst = sm_p + s * G::kPackedStage;
-          if (kt >= (uint32_t)PS && !wait(bar_p_empty + 8 * s, (kt / PS - 1) & 1)) return false;
-          const int rows = min(kKeys, g.Lc - t * kKeys), first = min(rows, 64), second = rows - first;
-          const size_t row = (size_t)z * p.capacity + (size_t)t * kKeys;
-          mbar_expect_tx(bar, Pk::bytes(first) + (second > 0 ? Pk::bytes(second) : 0u));
-          Pk::copy(dst, p.k, p.k_scale, row, first, bar);
-          if (second > 0) Pk::copy(dst + Pk::kBytes, p.k, p.k_scale, row + 64, second, bar);
-          ++kt;
-        } else {
-          const uint32_t i = tiles[w], s = 2 * w + (i & 1), bar = bar_k_full + 8 * s;
-          if (i >= 2 && !wait(bar_k_empty + 8 * s, ((i >> 1) - 1) & 1)) return false;
-          mbar_expect_tx(bar, (uint32_t)p.k_box * 128u * G::kPanels);
-          for (int pn = 0; pn < G::kPanels; ++pn) tma_load_3d(sm_k + s * G::kTile + pn * G::kPanel, &tm_k, bar, pn * 64, t * kKeys, z);
-          ++tiles[w];
-        }
-        return true;
-      };
-      while (ok && walk.next(g)) {
-        if (resident)
-          for (int c = 0; c < p.n_qc && ok; ++c) ok = load_q(c);
-        for (int t = g.begin; t < g.end && ok; t += 2) {
-          ok = load_k(t, 0);
-          if (ok && t + 1 < g.end) ok = load_k(t + 1, 1);
-          if (!resident)
-            for (int c = 0; c < p.n_qc && ok; ++c) ok = load_q(c);
-        }
+        for (int pn = 0; pn < G::kPanels; ++pn) tma_load_3d(sm_q + s * q_slot + pn * p.q_panel, &tm_q, bar_q_tx + 8 * s, pn * 64, c * kRows, z);
       }
-      // no copy lands after the block has released its shared memory
+      __syncwarp();
+      ++ev;
+      return true;
+    };
+    auto load_k = [&](int t, int w) {
+      const int z = ((g.layer + p.layer_begin) * p.batch + g.b) * p.n_kv_heads + g.kvh;
       if (kQ4) {
-        for (uint32_t i = kt > (uint32_t)PS ? kt - PS : 0; i < kt; ++i) mbar_wait(bar_p_full + 8 * (i % PS), (i / PS) & 1, never_ptr);
+        const uint32_t s = ps.stage, bar = bar_p_full + 8 * s;
+        if (kt >= PS && !wait(bar_p_empty + 8 * s, ps.parity ^ 1u)) return false;
+        const int rows = min(kKeys, g.Lc - t * kKeys);
+        if (lane == 0) mbar_expect_tx(bar, Pk::bytes(rows));
+        __syncwarp();
+        if (lane < 2) Pk::copy_part(sm_p + s * G::kPackedStage, p.k, p.k_scale, lane, (size_t)z * p.capacity + (size_t)t * kKeys, rows, bar);
+        __syncwarp();
+        ++kt;
+        ps.advance(PS);
       } else {
-        for (int w = 0; w < 2; ++w)
-          for (uint32_t i = tiles[w] > 2 ? tiles[w] - 2 : 0; i < tiles[w]; ++i) mbar_wait(bar_k_full + 8 * (2 * w + (i & 1)), (i >> 1) & 1, never_ptr);
+        const uint32_t i = tiles[w], s = 2 * w + (i & 1), bar = bar_k_full + 8 * s;
+        if (i >= 2 && !wait(bar_k_empty + 8 * s, ((i >> 1) - 1) & 1)) return false;
+        if (lane == 0) mbar_expect_tx(bar, (uint32_t)p.k_box * 128u * G::kPanels);
+        __syncwarp();
+        if (lane < G::kPanels) tma_load_3d(sm_k + s * G::kTile + lane * G::kPanel, &tm_k, bar, lane * 64, t * kKeys, z);
+        __syncwarp();
+        ++tiles[w];
       }
-      for (uint32_t i = ev > 2 ? ev - 2 : 0; i < ev; ++i) mbar_wait(bar_q_tx + 8 * (i & 1), (i >> 1) & 1, never_ptr);
+      return true;
+    };
+    while (ok && walk.next(g)) {
+      if (resident)
+        for (int c = 0; c < p.n_qc && ok; ++c) ok = load_q(c);
+      for (int t = g.begin; t < g.end && ok; t += 2) {
+        ok = load_k(t, 0);
+        if (ok && t + 1 < g.end) ok = load_k(t + 1, 1);
+        if (!resident)
+          for (int c = 0; c < p.n_qc && ok; ++c) ok = load_q(c);
+      }
     }
-  } else if (warp == 13 || warp == 14) {
+    // no copy lands after the block has released its shared memory
+    if (kQ4) {
+      for (uint32_t i = kt > PS ? kt - PS : 0; i < kt; ++i) mbar_wait(bar_p_full + 8 * (i % PS), (i / PS) & 1, never_ptr);
+    } else {
+      for (int w = 0; w < 2; ++w)
+        for (uint32_t i = tiles[w] > 2 ? tiles[w] - 2 : 0; i < tiles[w]; ++i) mbar_wait(bar_k_full + 8 * (2 * w + (i & 1)), (i >> 1) & 1, never_ptr);
+    }
+    for (uint32_t i = ev > 2 ? ev - 2 : 0; i < ev; ++i) mbar_wait(bar_q_tx + 8 * (i & 1), (i >> 1) & 1, never_ptr);
+  } else if (warp == kControl + 1 || warp == kControl + 2) {
     if (elect_one_sync()) {
       // ================================================================= MMA issuers, one for each group of warps
-      const int w = warp - 13;
+      const int w = warp - kControl - 1;
       auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait(bar, parity, abort_ptr); };
       uint32_t kt = 0, ev = 0, st = 0;   // the group's tiles, events, the group's steps so far
       const uint64_t desc_k0 = make_smem_desc_sw128(sm_k, 16, 1024), desc_q0 = make_smem_desc_sw128(sm_q, 16, 1024);
@@ -246,12 +267,12 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
               if (!ok) break;
               tc_fence_after_sync();
               const uint32_t idesc = make_idesc_bf16(128, (uint32_t)((chunk_rows(c) + 15) & ~15), 0);
-              const uint64_t dk = desc_offset(desc_k0, ks * G::kTile), dq = desc_offset(desc_q0, (e & 1) * G::kTile);
+              const uint64_t dk = desc_offset(desc_k0, ks * G::kTile), dq = desc_offset(desc_q0, (e & 1) * q_slot);
               const uint32_t d = tmem + w * 256 + b * kRows;
 #pragma unroll
               for (int k = 0; k < D / 16; ++k) {
-                const uint32_t off = ((k >> 2) * G::kPanel + (k & 3) * 32) >> 4;
-                mma_ss_lo<false>(d, (uint32_t)dk + off, (uint32_t)dq + off, (uint32_t)(dk >> 32), idesc, k > 0 ? 1u : 0u);
+                const uint32_t a = ((k >> 2) * G::kPanel + (k & 3) * 32) >> 4, b_off = ((k >> 2) * p.q_panel + (k & 3) * 32) >> 4;
+                mma_ss_lo<false>(d, (uint32_t)dk + a, (uint32_t)dq + b_off, (uint32_t)(dk >> 32), idesc, k > 0 ? 1u : 0u);
               }
               tc_commit(bar_s_ready + buf);
               ++st;
@@ -275,7 +296,7 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       tc_commit(bar_drain + 8 * w);
       mbar_wait(bar_drain + 8 * w, 0, never_ptr);
     }
-  } else if (warp == 15) {
+  } else if (warp == kControl + 3) {
     // ================================================================= query rows: logarithms, zeros
     uint32_t ev = 0;
     while (ok && walk.next(g)) {
@@ -302,23 +323,24 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           logs[s * kRows + r] = out[j] ? -CUDART_INF_F : x[j] * -1.4426950408889634f;
           // a row that takes no part: 0 * scale - inf, whatever it holds
           for (uint32_t todo = __ballot_sync(0xffffffffu, out[j] && r < n16); todo != 0; todo &= todo - 1)
-            if (lane < D / 8) q4::clear_piece<D>(sm_q + s * G::kTile, G::kPanel, (j * 32 + __ffs(todo) - 1) * (D / 8) + lane);
+            if (lane < D / 8) q4::clear_piece<D>(sm_q + s * q_slot, p.q_panel, (j * 32 + __ffs(todo) - 1) * (D / 8) + lane);
         }
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_q_ready + 8 * s);
       }
     }
-  } else if (warp >= 8) {
-    if (kQ4) {
-      // ================================================================= decoders: two warps for either group's tiles
-      constexpr int kGroups = D / q4::kGroup, kPer = kKeys * kGroups / 64, kBatch = 4;
-      const int me = tid & 63, w = (warp - 8) >> 1;
-      uint32_t kt = 0, n = 0;   // tiles, the group's tiles
+  } else if (warp >= kSumWarps) {
+    if constexpr (kQ4) {
+      // ================================================================= decoders, four warps for either group's tiles
+      constexpr int kTeam = G::kDecodeWarps / 2 * 32, kGroups = D / q4::kGroup, kPer = kKeys * kGroups / kTeam, kBatch = 2;
+      const int me = tid & (kTeam - 1), w = (warp - kSumWarps) / (G::kDecodeWarps / 2);
+      uint32_t n = 0;   // the group's tiles
+      Ring ps;
       while (ok && walk.next(g)) {
-        for (int t = g.begin; t < g.end && ok; ++t, ++kt) {
-          const uint32_t s = kt % PS, packed = sm_p + s * G::kPackedStage;
-          ok = mbar_wait_warp(bar_p_full + 8 * s, (kt / PS) & 1, abort_ptr);
+        for (int t = g.begin; t < g.end && ok; ++t, ps.advance(PS)) {
+          const uint32_t s = ps.stage, packed = sm_p + s * G::kPackedStage;
+          ok = mbar_wait_warp(bar_p_full + 8 * s, ps.parity, abort_ptr);
           if (!ok) break;
           if (((t - g.begin) & 1) != w) {
             __syncwarp();
@@ -327,50 +349,54 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           }
           const uint32_t ks = 2 * w + (n & 1), tile = sm_k + ks * G::kTile;
           const int tasks = min(kKeys, g.Lc - t * kKeys) * kGroups;
-#pragma unroll
+          if (n >= 2) ok = mbar_wait_warp(bar_k_empty + 8 * ks, ((n >> 1) - 1) & 1, abort_ptr);
+          if (!ok) break;
+          // (a short loop: unrolled, it and the sums' code drive each other out of the instruction caches)
+#pragma unroll 1
           for (int i0 = 0; i0 < kPer; i0 += kBatch) {
             q4::Group32 x[kBatch];
 #pragma unroll
             for (int i = 0; i < kBatch; ++i) {
-              const int task = me + (i0 + i) * 64, half = task / (64 * kGroups);
-              if (task < tasks) x[i] = q4::read_group<D>(packed + half * Pk::kBytes, task - half * 64 * kGroups);
-            }
-            if (i0 + kBatch == kPer) {
-              __syncwarp();
-              if (lane == 0) mbar_arrive(bar_p_empty + 8 * s);
-            }
-            if (i0 == 0 && n >= 2) {
-              ok = mbar_wait_warp(bar_k_empty + 8 * ks, ((n >> 1) - 1) & 1, abort_ptr);
-              if (!ok) break;
+              const int task = me + (i0 + i) * kTeam;
+              if (task < tasks) x[i] = q4::read_group<D, kKeys>(packed, task);
             }
 #pragma unroll
             for (int i = 0; i < kBatch; ++i) {
-              const int task = me + (i0 + i) * 64;
+              const int task = me + (i0 + i) * kTeam;
               if (task < tasks) q4::write_group<D>(tile, G::kPanel, task, x[i]);
             }
           }
-          if (!ok) break;
           ++n;
           fence_proxy_async_smem();
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar_k_full + 8 * ks);
+          if (lane == 0) {
+            mbar_arrive(bar_p_empty + 8 * s);
+            mbar_arrive(bar_k_full + 8 * ks);
+          }
         }
       }
     }
   } else {
     // ================================================================= sums: thread = key of the tile = TMEM lane
-    const int w = warp >> 2, key = (warp & 3) * 32 + lane;
+    const int w = warp >> 2 & 1, half = warp >> 3, key = (warp & 3) * 32 + lane;
     const uint32_t t_s = tmem + ((uint32_t)((warp & 3) * 32) << 16) + w * 256;
     const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2);
-    uint32_t ev = 0, st = 0;
+    uint32_t ev = 0, st = 0, kt = 0;   // events, the group's steps and tiles
     while (ok && walk.next(g)) {
       const size_t row0 = (((size_t)(g.layer + p.layer_begin) * p.batch + g.b) * p.n_kv_heads + g.kvh) * p.capacity;
+      // what the group's next tile has collected so far, asked for a tile ahead: a load from memory takes longer than a tile
+      auto collected_of = [&](int t) {
+        const int j = t * kKeys + key;
+        return half == 0 && t < g.end && j < g.Lc && p.collected && p.decay != 0.f ? p.collected[row0 + j] : 0.f;
+      };
+      float ahead = collected_of(g.begin + w);
       for (int t0 = g.begin; t0 < g.end && ok; t0 += 2) {
         const int t = t0 + w;
         if (t < g.end) {
           float a0 = 0.f, a1 = 0.f, a2 = 0.f, a3 = 0.f;
           const int j = t * kKeys + key;
-          const float before = j < g.Lc && p.collected && p.decay != 0.f ? p.decay * p.collected[row0 + j] : 0.f;
+          const float before = ahead;
+          ahead = collected_of(t + 2);
           for (int c = 0; c < p.n_qc && ok; ++c, ++st) {
             const uint32_t e = ev + c, b = st & 1, buf = 16 * w + 8 * b;
             const int n16 = (chunk_rows(c) + 15) & ~15;
@@ -378,12 +404,14 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             if (ok) ok = mbar_wait_warp(bar_q_ready + 8 * (e & 1), (e >> 1) & 1, abort_ptr);
             if (!ok) break;
             tc_fence_after_sync();
+            // this half's columns, 16 at a time
+            const int mid = ((n16 >> 4) + 1 >> 1) << 4, first = half ? mid : 0, last = half ? n16 : mid;
             const uint32_t from = t_s + b * kRows, log_at = sm_log + (e & 1) * kRows * 4;
-            auto add = [&](const uint32_t* v, uint32_t at, int n) {
+            auto add = [&](const uint32_t* v, int i0, int n) {
 #pragma unroll
               for (int i = 0; i < 32; i += 4) {
                 if (i >= n) break;
-                const float4 l = ld_shared_f4(at + i * 4);
+                const float4 l = ld_shared_f4(log_at + (i0 + i) * 4);
                 float x0, x1, x2, x3;
                 unpack2(fma2(pack2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), scale2, pack2(l.x, l.y)), x0, x1);
                 unpack2(fma2(pack2(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])), scale2, pack2(l.z, l.w)), x2, x3);
@@ -394,16 +422,17 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
               }
             };
             uint32_t v[32];
+            int i = first;
 #pragma unroll 1
-            for (int i = 0; i + 32 <= n16; i += 32) {
+            for (; i + 32 <= last; i += 32) {
               tmem_ld32(from + i, v);
               tmem_ld_wait();
-              add(v, log_at + i * 4, 32);
+              add(v, i, 32);
             }
-            if (n16 & 16) {
-              tmem_ld16(from + (n16 & ~31), v);
+            if (i < last) {
+              tmem_ld16(from + i, v);
               tmem_ld_wait();
-              add(v, log_at + (n16 & ~31) * 4, 16);
+              add(v, i, 16);
             }
             __syncwarp();
             if (lane == 0) {
@@ -412,7 +441,21 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
               if (!resident) mbar_arrive(bar_q_empty + 8 * (e & 1));
             }
           }
-          if (ok && j < g.Lc) p.weight[row0 + j] = before + ((a0 + a1) + (a2 + a3));
+          if (!ok) break;
+          // Four tiles' parts are kept: the second half is never that far ahead, since a score buffer waits for both halves, and the
+          // first half has read a tile's part before it releases a buffer of its next tile.
+          const float sum = (a0 + a1) + (a2 + a3);
+          float* const part = parts + (w * 4 + (kt & 3)) * kKeys + key;
+          const uint32_t bar = bar_part + (w * 4 + (kt & 3)) * 8;
+          if (half) {
+            *part = sum;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar);
+          } else {
+            ok = mbar_wait_warp(bar, (kt >> 2) & 1, abort_ptr);
+            if (ok && j < g.Lc) p.weight[row0 + j] = fmaf(p.decay, before, sum + *part);
+          }
+          ++kt;
         } else if (!resident) {   // no second tile: the query rows are not needed here
           for (int c = 0; c < p.n_qc && ok; ++c) {
             ok = mbar_wait_warp(bar_q_ready + 8 * ((ev + c) & 1), ((ev + c) >> 1) & 1, abort_ptr);
@@ -437,7 +480,7 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   tc_fence_before_sync();
   __syncthreads();
   if (tid == 0 && (*abort_ptr || *never_ptr)) dlm_set_status(p.status, DLM_ERR_TIMEOUT);
-  if (warp == 13) {
+  if (warp == kControl + 1) {
     tc_fence_after_sync();
     tmem_dealloc(tmem, kTmemCols);
     __syncwarp();
@@ -460,15 +503,12 @@ int accumulate(dlm_ctx* ctx, const Cache* cache, const uint8_t* k_scale, int lay
   if (units * tiles >= (1LL << 30)) return DLM_ERR_UNSUPPORTED;   // items are counted in 32 bits
   DLM_DEVICE_TRY(ctx);
   const Kernel kern = D == 128 ? cache_weight_kernel<128, kQ4> : cache_weight_kernel<64, kQ4>;
+  const int threads = Shape<128, kQ4>::kThreads;
   const int which = (D == 128 ? 0 : 1) + (kQ4 ? 2 : 0);
   if (ctx->weight_smem_limit[which] == 0) {
     DLM_CUDA_TRY(cudaFuncSetAttribute(reinterpret_cast<const void*>(kern), cudaFuncAttributeMaxDynamicSharedMemorySize, ctx->max_smem_optin));
     ctx->weight_smem_limit[which] = ctx->max_smem_optin;
   }
-  const int tiles_bytes = D == 128 ? Shape<128>::kTiles + (kQ4 ? Shape<128>::PS * Shape<128>::kPackedStage : 0)
-                                   : Shape<64>::kTiles + (kQ4 ? Shape<64>::PS * Shape<64>::kPackedStage : 0);
-  const int smem = 1024 + tiles_bytes + Shape<64>::kLogBytes + kBarrierBytes + kFlagBytes + 4 * length_ints(cache->batch);
-  if (smem > ctx->max_smem_optin) return DLM_ERR_UNSUPPORTED;
   Params p;
   p.cache_len = cache->cache_len;
   p.q_len = q_len;
@@ -490,6 +530,15 @@ int accumulate(dlm_ctx* ctx, const Cache* cache, const uint8_t* k_scale, int lay
   p.n_qc = (p.rows_total + kRows - 1) / kRows;
   p.q_box = p.rows_total < kRows ? p.rows_total : kRows;
   p.k_box = cache->capacity < kKeys ? cache->capacity : kKeys;
+  p.q_panel = (uint32_t)((p.q_box + 15) & ~15) * 128u;
+  const int tile = D == 128 ? Shape<128, kQ4>::kTile : Shape<64, kQ4>::kTile;
+  const int packed = D == 128 ? Shape<128, kQ4>::kPackedStage : Shape<64, kQ4>::kPackedStage;
+  const int fixed = 1024 + Shape<128, kQ4>::KS * tile + 2 * (D / 64) * (int)p.q_panel + kLogBytes + kPartBytes + kBarrierBytes + kFlagBytes +
+                    4 * length_ints(cache->batch);
+  p.n_packed = kQ4 ? (ctx->max_smem_optin - fixed) / packed : 0;
+  if (p.n_packed > kMaxPacked) p.n_packed = kMaxPacked;
+  const int smem = fixed + p.n_packed * packed;
+  if (smem > ctx->max_smem_optin || (kQ4 && p.n_packed < 2)) return DLM_ERR_UNSUPPORTED;
   p.by_kv_heads = make_fast_div(p.n_kv_heads);
   p.by_q_cap = make_fast_div(q_cap);
   p.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;
@@ -501,7 +550,7 @@ int accumulate(dlm_ctx* ctx, const Cache* cache, const uint8_t* k_scale, int lay
     rc = encode_rows_map(ctx, &tm_k, cache->k, D, cache->capacity, (long long)cache->n_layers * cache->batch * cache->n_kv_heads, p.k_box);
   if (rc != DLM_OK) return rc;
   const int sms = ctx->num_sms < kMaxGrid ? ctx->num_sms : kMaxGrid, grid = units * tiles < sms ? (int)(units * tiles) : sms;
-  DLM_CUDA_TRY(dlm_launch(kern, dim3(grid), dim3(kThreads), (size_t)smem, static_cast<cudaStream_t>(stream), tm_q, tm_k, p));
+  DLM_CUDA_TRY(dlm_launch(kern, dim3(grid), dim3(threads), (size_t)smem, static_cast<cudaStream_t>(stream), tm_q, tm_k, p));
   return dlm_launch_ok(ctx, 1);
 }
 

@@ -61,7 +61,7 @@ struct Deal {
   __device__ __forceinline__ int lo(int c) const { return share * c + (rem * c) / n; }
   // the block that has an item
   __device__ __forceinline__ int owner(int item) const {
-    int c = min(n - 1, (int)(((long long)item * n) / max(total, 1)));
+    int c = min(n - 1, (int)(__fdividef((float)item, (float)max(total, 1)) * (float)n));   // to within a block or two
     while (lo(c) > item) --c;
     while (lo(c + 1) <= item) ++c;
     return c;

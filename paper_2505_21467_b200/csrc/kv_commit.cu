@@ -17,11 +17,14 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kUnroll = 4;
+// 4-bit cache: an item is two vectors (8 values each) of a row, one from either half of it, so that decoding an item's number, as
+// much work as quantising a vector, is shared by twice as many values; half as many items are in flight a thread.
+constexpr int kUnrollQ4 = 2;
 
 struct CommitParams {
-  void* cache_k;         // 16-byte vectors; 4-bit cache: a 32-bit word for each vector of a source row
+  void* cache_k;         // 16-byte vectors; 4-bit cache: a 32-bit word for each vector of a source row, a scale byte for every fourth
   void* cache_v;
-  uint8_t* k_scale;      // 4-bit cache: a byte for every fourth
+  uint8_t* k_scale;
   uint8_t* v_scale;
   int32_t* cache_len;
   const uint4* k_new;
@@ -31,7 +34,7 @@ struct CommitParams {
   const int32_t* n_rows;
   int n_max, src_len, advance_len, layer_begin, n_layers_call, dst_mode;
   int batch, n_kv_heads, capacity;
-  int vec_per_row;       // head_dim * 2 / 16
+  int vec_per_row;       // items of a row: its vectors of 16 bytes; 4-bit cache: half of them
   FastDiv by_vec, by_rows, by_heads, by_batch;   // vec_per_row, n_max, n_kv_heads, batch
   long long n_items;     // n_layers_call * batch * heads * n_max * vec_per_row
   long long per_block;   // items per block (a multiple of 32)
@@ -51,12 +54,13 @@ __device__ __forceinline__ int valid_rows(const CommitParams& p, int b, int len0
 // Where one item comes from and goes to (vector indices), or to = -1: nothing to move.
 struct Move {
   long long from, to;
+  int vec;   // number of the item in its row
 };
 
 // Idx int: item numbers below 2^31, decoded with host-prepared reciprocals.
 template <typename Idx>
 __device__ __forceinline__ Move find_move(const CommitParams& p, Idx item) {
-  Move mv = {0, -1};
+  Move mv = {0, -1, 0};
   int vec, r, h, b, lc;   // vector of the row, row, head, batch element, layer within the call
   if (sizeof(Idx) == 4) {
     lc = p.by_batch.divmod(p.by_heads.divmod(p.by_rows.divmod(p.by_vec.divmod((int)item, vec), r), h), b);
@@ -87,6 +91,7 @@ __device__ __forceinline__ Move find_move(const CommitParams& p, Idx item) {
     if (vec == 0 && h == 0 && lc == 0) dlm_set_status(p.status, DLM_ERR_INDEX);
     return mv;
   }
+  mv.vec = vec;
   mv.from = ((((long long)lc * p.batch + b) * p.n_kv_heads + h) * p.src_len + src) * p.vec_per_row + vec;
   mv.to = ((((long long)(lc + p.layer_begin) * p.batch + b) * p.n_kv_heads + h) * p.capacity + dst) * p.vec_per_row + vec;
   return mv;
@@ -112,24 +117,51 @@ __device__ __forceinline__ void advance_when_last(const CommitParams& p) {
   if (threadIdx.x == 0) *p.ticket = 0;
 }
 
-// The vectors kk and vv to where `to` says (vector number in the cache, -1: nowhere).  4-bit cache: four neighbouring lanes have a
-// group of 32 values, which lies in one row (a row's vectors are a multiple of four), so all four have a destination or none has;
-// every lane of the warp calls this.
+// What an item brings: vectors of K and of V.
 template <bool kQ4>
-__device__ __forceinline__ void store_rows(const CommitParams& p, long long to, const uint4& kk, const uint4& vv) {
+struct Item {
+  uint4 k[kQ4 ? 2 : 1], v[kQ4 ? 2 : 1];
+};
+// 4 bits: number of an item's first vector (or of its word in the cache), given row * (items of a row) + item in the row
+__device__ __forceinline__ long long first_vector(long long at, int vec) { return 2 * at - vec; }
+
+template <bool kQ4>
+__device__ __forceinline__ void load_item(const CommitParams& p, const Move& mv, Item<kQ4>& x) {
+  if (mv.to < 0) {
+    if (kQ4) x.k[0] = x.v[0] = x.k[kQ4 ? 1 : 0] = x.v[kQ4 ? 1 : 0] = make_uint4(0, 0, 0, 0);
+    return;
+  }
+  const long long at = kQ4 ? first_vector(mv.from, mv.vec) : mv.from;
+  x.k[0] = __ldcs(p.k_new + at);
+  x.v[0] = __ldcs(p.v_new + at);
   if (kQ4) {
-    uint32_t kb, vb;
-    const uint32_t kw = q4::encode8(kk, kb), vw = q4::encode8(vv, vb);
-    if (to < 0) return;
-    static_cast<uint32_t*>(p.cache_k)[to] = kw;
-    static_cast<uint32_t*>(p.cache_v)[to] = vw;
-    if ((to & 3) == 0) {
-      p.k_scale[to >> 2] = (uint8_t)kb;
-      p.v_scale[to >> 2] = (uint8_t)vb;
+    x.k[kQ4 ? 1 : 0] = __ldcs(p.k_new + at + p.vec_per_row);
+    x.v[kQ4 ? 1 : 0] = __ldcs(p.v_new + at + p.vec_per_row);
+  }
+}
+
+// 4-bit cache: four neighbouring lanes have a group of 32 values, which lies in one row (a row's items are a multiple of four), so all four
+// have a destination or none has; every lane of the warp calls this.
+template <bool kQ4>
+__device__ __forceinline__ void store_item(const CommitParams& p, const Move& mv, const Item<kQ4>& x) {
+  if (kQ4) {
+    const long long at = first_vector(mv.to, mv.vec);
+#pragma unroll
+    for (int h = 0; h < (kQ4 ? 2 : 1); ++h) {
+      uint32_t kb, vb;
+      const uint32_t kw = q4::encode8(x.k[h], kb), vw = q4::encode8(x.v[h], vb);
+      if (mv.to < 0) continue;
+      const long long to = at + h * p.vec_per_row;
+      static_cast<uint32_t*>(p.cache_k)[to] = kw;
+      static_cast<uint32_t*>(p.cache_v)[to] = vw;
+      if ((mv.vec & 3) == 0) {
+        p.k_scale[to >> 2] = (uint8_t)kb;
+        p.v_scale[to >> 2] = (uint8_t)vb;
+      }
     }
-  } else if (to >= 0) {
-    static_cast<uint4*>(p.cache_k)[to] = kk;
-    static_cast<uint4*>(p.cache_v)[to] = vv;
+  } else if (mv.to >= 0) {
+    static_cast<uint4*>(p.cache_k)[mv.to] = x.k[0];
+    static_cast<uint4*>(p.cache_v)[mv.to] = x.v[0];
   }
 }
 
@@ -139,25 +171,20 @@ __global__ void __launch_bounds__(kThreads, 4) kv_commit_kernel(const __grid_con
   dlm_trigger_dependents();
   const Idx begin = (Idx)blockIdx.x * (Idx)p.per_block;
   const Idx end = (Idx)min((long long)begin + p.per_block, p.n_items);
+  constexpr int kAtOnce = kQ4 ? kUnrollQ4 : kUnroll;
   // (4 bits: the lanes of a warp leave together)
-  for (Idx base = begin + (Idx)threadIdx.x; kQ4 ? (base & ~(Idx)31) < end : base < end; base += (Idx)(kThreads * kUnroll)) {
-    uint4 kk[kUnroll], vv[kUnroll];
-    long long to[kUnroll];
+  for (Idx base = begin + (Idx)threadIdx.x; kQ4 ? (base & ~(Idx)31) < end : base < end; base += (Idx)(kThreads * kAtOnce)) {
+    Item<kQ4> x[kAtOnce];
+    Move mv[kAtOnce];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      to[u] = -1;
-      if (kQ4) kk[u] = vv[u] = make_uint4(0, 0, 0, 0);
+    for (int u = 0; u < kAtOnce; ++u) {
+      mv[u] = {0, -1, 0};
       const Idx item = base + (Idx)(u * kThreads);
-      if (item >= end) continue;
-      const Move mv = find_move<Idx>(p, item);
-      to[u] = mv.to;
-      if (mv.to >= 0) {
-        kk[u] = __ldcs(p.k_new + mv.from);
-        vv[u] = __ldcs(p.v_new + mv.from);
-      }
+      if (item < end) mv[u] = find_move<Idx>(p, item);
+      load_item<kQ4>(p, mv[u], x[u]);
     }
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) store_rows<kQ4>(p, to[u], kk[u], vv[u]);
+    for (int u = 0; u < kAtOnce; ++u) store_item<kQ4>(p, mv[u], x[u]);
   }
   if (p.advance_len) advance_when_last(p);
 }
@@ -171,19 +198,16 @@ __global__ void __launch_bounds__(kThreads) kv_commit_small_kernel(const __grid_
   dlm_grid_dependency_wait();
   dlm_trigger_dependents();
   const int item = (int)blockIdx.x * kThreads + (int)threadIdx.x;
-  Move mv = {0, -1};
+  Move mv = {0, -1, 0};
   if (item < (int)p.n_items) mv = find_move<int>(p, item);
-  uint4 kk = make_uint4(0, 0, 0, 0), vv = kk;
-  if (mv.to >= 0) {
-    kk = __ldcs(p.k_new + mv.from);
-    vv = __ldcs(p.v_new + mv.from);
-  }
+  Item<kQ4> x;
+  load_item<kQ4>(p, mv, x);
   if (p.advance_len) advance_when_last(p);
-  store_rows<kQ4>(p, mv.to, kk, vv);
+  store_item<kQ4>(p, mv, x);
 }
 
-// Rows of the 4-bit cache as bf16: one item is 8 values of a K row and of the V row, a 32-bit word and a scale byte each.  Bound by HBM
-// like the commit; items, decoding and the words' coalescing are the commit's.
+// Rows of the 4-bit cache as bf16: one item is 2 x 8 values of a K row and of the V row, a 32-bit word and a scale byte each.  Bound by
+// HBM like the commit; items, decoding and the words' coalescing are the commit's.
 struct ReadParams {
   const uint32_t* k;
   const uint32_t* v;
@@ -204,11 +228,12 @@ __global__ void __launch_bounds__(kThreads) kv_read_q4_kernel(const __grid_const
   dlm_grid_dependency_wait();
   dlm_trigger_dependents();
   const Idx step = (Idx)gridDim.x * kThreads;
-  for (Idx base = (Idx)blockIdx.x * kThreads + (Idx)threadIdx.x; base < (Idx)p.n_items; base += step * kUnroll) {
-    uint32_t kw[kUnroll], vw[kUnroll], kb[kUnroll], vb[kUnroll];
-    bool on[kUnroll];
+  for (Idx base = (Idx)blockIdx.x * kThreads + (Idx)threadIdx.x; base < (Idx)p.n_items; base += step * kUnrollQ4) {
+    uint32_t kw[kUnrollQ4][2], vw[kUnrollQ4][2], kb[kUnrollQ4][2], vb[kUnrollQ4][2];
+    long long to[kUnrollQ4];
+    bool on[kUnrollQ4];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
+    for (int u = 0; u < kUnrollQ4; ++u) {
       const Idx item = base + (Idx)u * step;
       on[u] = item < (Idx)p.n_items;
       if (!on[u]) continue;
@@ -239,21 +264,27 @@ __global__ void __launch_bounds__(kThreads) kv_read_q4_kernel(const __grid_const
         on[u] = false;
       }
       if (!on[u]) continue;
-      const long long at = ((((long long)(lc + p.layer_begin) * p.batch + b) * p.n_kv_heads + h) * p.capacity + row) * p.vec_per_row + vec;
-      kw[u] = p.k[at];
-      vw[u] = p.v[at];
-      kb[u] = p.k_scale[at >> 2];
-      vb[u] = p.v_scale[at >> 2];
+      const long long at = first_vector(((((long long)(lc + p.layer_begin) * p.batch + b) * p.n_kv_heads + h) * p.capacity + row) * p.vec_per_row + vec, vec);
+      to[u] = first_vector((long long)item, vec);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        kw[u][i] = p.k[at + i * p.vec_per_row];
+        vw[u][i] = p.v[at + i * p.vec_per_row];
+        kb[u][i] = p.k_scale[(at + i * p.vec_per_row) >> 2];
+        vb[u][i] = p.v_scale[(at + i * p.vec_per_row) >> 2];
+      }
     }
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
+    for (int u = 0; u < kUnrollQ4; ++u) {
       if (!on[u]) continue;
-      const Idx item = base + (Idx)u * step;
-      uint32_t w[4];
-      q4::decode8(kw[u], q4::make_scale(kb[u]), w);
-      p.k_out[item] = make_uint4(w[0], w[1], w[2], w[3]);
-      q4::decode8(vw[u], q4::make_scale(vb[u]), w);
-      p.v_out[item] = make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        uint32_t w[4];
+        q4::decode8(kw[u][i], q4::make_scale(kb[u][i]), w);
+        __stcs(p.k_out + to[u] + i * p.vec_per_row, make_uint4(w[0], w[1], w[2], w[3]));
+        q4::decode8(vw[u][i], q4::make_scale(vb[u][i]), w);
+        __stcs(p.v_out + to[u] + i * p.vec_per_row, make_uint4(w[0], w[1], w[2], w[3]));
+      }
     }
   }
 }
@@ -292,7 +323,7 @@ int commit(dlm_ctx* ctx, const Cache* cache, uint8_t* k_scale, uint8_t* v_scale,
   p.batch = cache->batch;
   p.n_kv_heads = cache->n_kv_heads;
   p.capacity = cache->capacity;
-  p.vec_per_row = cache->head_dim * 2 / 16;
+  p.vec_per_row = cache->head_dim * 2 / 16 / (kQ4 ? 2 : 1);
   p.by_vec = make_fast_div(p.vec_per_row);
   p.by_rows = make_fast_div(n_max);
   p.by_heads = make_fast_div(cache->n_kv_heads);
@@ -318,7 +349,7 @@ int commit(dlm_ctx* ctx, const Cache* cache, uint8_t* k_scale, uint8_t* v_scale,
     DLM_CUDA_TRY(dlm_launch(kv_commit_small_kernel<kQ4>, dim3(blocks), dim3(kThreads), 0, st, p));
     return dlm_launch_ok(ctx, 1);
   }
-  const long long per_pass = (long long)kThreads * kUnroll;
+  const long long per_pass = (long long)kThreads * (kQ4 ? kUnrollQ4 : kUnroll);
   long long blocks = (p.n_items + per_pass - 1) / per_pass;
   if (blocks > max_blocks) blocks = max_blocks;
   p.per_block = ((p.n_items + blocks - 1) / blocks + 31) & ~31LL;
@@ -375,7 +406,7 @@ extern "C" int dlm_kv_cache_read_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* cache, 
   p.batch = cache->batch;
   p.n_kv_heads = cache->n_kv_heads;
   p.capacity = cache->capacity;
-  p.vec_per_row = cache->head_dim / 8;
+  p.vec_per_row = cache->head_dim / 16;
   p.by_vec = make_fast_div(p.vec_per_row);
   p.by_rows = make_fast_div(n_max);
   p.by_heads = make_fast_div(cache->n_kv_heads);

@@ -15,6 +15,8 @@
 #include <cuda_bf16.h>
 #include <stdint.h>
 
+#include "sm100_ptx.cuh"
+
 namespace q4 {
 
 constexpr int kGroup = 32;
@@ -75,19 +77,20 @@ __device__ __forceinline__ uint32_t encode8(uint4 raw, uint32_t& byte) {
   const int e = (int)((tb + 0x7FFFFu + ((tb >> 20) & 1u)) >> 20) - (int)((127u - 20u) << 3);
   byte = (uint32_t)min(max(e, 0), 255);
   const float s = __uint_as_float(scale_bf16(byte) << 16), inv = __fdividef(1.f, s);
-  uint32_t word = 0;
+  const uint64_t inv2 = sm100::pack2(inv, inv), minus_s2 = sm100::pack2(-s, -s), magic2 = sm100::pack2(12582920.f, 12582920.f);
+  uint32_t n[2][4];   // 1.5 * 2^23 + 8 + quotient as a float: its last bits are the rounded quotient + 8
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    uint32_t n[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const float x = __uint_as_float(h ? w[i] & 0xFFFF0000u : w[i] << 16);
-      const float y = x * inv, z = fmaf(fmaf(-s, y, x), inv, y);
-      n[h] = __float_as_uint(z + 12582920.f) & 15u;   // 1.5 * 2^23 + 8: the sum's last bits are the rounded quotient + 8
-    }
-    word |= (n[0] << (4 * i)) | (n[1] << (16 + 4 * i));
+    const uint64_t x = sm100::pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+    const uint64_t y = sm100::mul2(x, inv2), z = sm100::fma2(sm100::fma2(minus_s2, y, x), inv2, y);
+    float lo, hi;
+    sm100::unpack2(sm100::add2(z, magic2), lo, hi);
+    n[0][i] = __float_as_uint(lo);
+    n[1][i] = __float_as_uint(hi);
   }
-  return word;
+  // (what is above those bits stays above bit 16 of the sums)
+  const uint32_t even = n[0][0] + (n[0][1] << 4) + (n[0][2] << 8) + (n[0][3] << 12), odd = n[1][0] + (n[1][1] << 4) + (n[1][2] << 8) + (n[1][3] << 12);
+  return __byte_perm(even, odd, 0x5410);
 }
 
 }  // namespace q4

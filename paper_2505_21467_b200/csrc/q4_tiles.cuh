@@ -6,18 +6,18 @@
 
 namespace q4 {
 
-// 64 consecutive rows of K or of V as copied: [64][D / 2] bytes of values, [64][D / 32] scale bytes.
-template <int D>
+// kRows consecutive rows of K or of V as copied: [kRows][D / 2] bytes of values, [kRows][D / 32] scale bytes.
+template <int D, int kRows>
 struct Packed {
-  static constexpr int kRows = 64;
   static constexpr int kRowBytes = D / 2, kRowScales = D / kGroup;
   static constexpr int kData = kRows * kRowBytes, kBytes = kData + kRows * kRowScales;
   // bytes that a copy of `rows` rows brings: whole 16-byte pieces of scales (rows up to the next multiple of 8, which the capacity is)
   __device__ static __forceinline__ uint32_t scale_bytes(int rows) { return (uint32_t)((rows * kRowScales + 15) & ~15); }
   __device__ static __forceinline__ uint32_t bytes(int rows) { return (uint32_t)(rows * kRowBytes) + scale_bytes(rows); }
-  __device__ static __forceinline__ void copy(uint32_t dst, const uint8_t* data, const uint8_t* scale, size_t row, int rows, uint32_t bar) {
-    sm100::bulk_load(dst, data + row * kRowBytes, (uint32_t)(rows * kRowBytes), bar);
-    sm100::bulk_load(dst + kData, scale + row * kRowScales, scale_bytes(rows), bar);
+  // One of the two copies that this takes, by one lane: a lane needs 200 - 300 cycles to issue a copy, so they are issued side by side.
+  __device__ static __forceinline__ void copy_part(uint32_t dst, const uint8_t* data, const uint8_t* scale, bool scales, size_t row, int rows, uint32_t bar) {
+    sm100::bulk_load(dst + (scales ? kData : 0), (scales ? scale : data) + row * (scales ? kRowScales : kRowBytes),
+                     scales ? scale_bytes(rows) : (uint32_t)(rows * kRowBytes), bar);
   }
 };
 
@@ -27,11 +27,11 @@ struct Group32 {
   uint32_t w[4];
   uint32_t scale;
 };
-template <int D>
+template <int D, int kRows>
 __device__ __forceinline__ Group32 read_group(uint32_t packed, int i) {
   Group32 g;
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(g.w[0]), "=r"(g.w[1]), "=r"(g.w[2]), "=r"(g.w[3]) : "r"(packed + i * 16) : "memory");
-  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(g.scale) : "r"(packed + Packed<D>::kData + i) : "memory");
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(g.scale) : "r"(packed + Packed<D, kRows>::kData + i) : "memory");
   return g;
 }
 
