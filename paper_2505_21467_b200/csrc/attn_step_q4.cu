@@ -324,11 +324,12 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     // nothing to store, so that its arrivals cannot run ahead into the stage's next phase.
     setmaxnreg_dec<kRegsDecode>();
     static_assert(PS % 2 == 0, "a packed stage belongs to one pair of teams");
-    constexpr int kThreadsOfTeam = G::kTeamWarps * 32, kTasks = kStep * (D / q4::kGroup), kPer = kTasks / kThreadsOfTeam, kBatch = 2;
+    constexpr int kThreadsOfTeam = G::kTeamWarps * 32;
     const int w = warp - (kThreads / 32 - 4 - G::kDecodeWarps), team = w / G::kTeamWarps, me = tid & (kThreadsOfTeam - 1);
     const bool is_k = team < 2, asks = (team & 1) == 0 && me == 0;
     const uint32_t odd = team & 1, stages = is_k ? KS : VS, tiles = is_k ? sm_k : sm_v, part = is_k ? 0 : Pk::kBytes;
     const uint32_t bar_full = is_k ? bar_k_full : bar_v_full, bar_empty = is_k ? bar_k_empty : bar_v_empty, bar_fresh = is_k ? bar_kf : bar_vf;
+    const q4::Decoder<D, kStep, kThreadsOfTeam> decoder(me, G::kPanel);
     auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_warp(bar, parity, abort_ptr, kLimit); };
     Walk walk(p, len, deal, blockIdx.x);
     Segment g = {};
@@ -376,22 +377,7 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             ok = wait(bar_empty + 8 * stage, (st / stages - 1) & 1);
             if (!ok) break;
           }
-          // (a short loop: unrolled, this code and the softmax's drive each other out of the instruction caches)
-          const int tasks = keys * (D / q4::kGroup);
-#pragma unroll 1
-          for (int i0 = 0; i0 < kPer; i0 += kBatch) {
-            q4::Group32 x[kBatch];
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-              const int task = me + (i0 + i) * kThreadsOfTeam;
-              if (task < tasks) x[i] = q4::read_group<D, kStep>(packed, task);
-            }
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-              const int task = me + (i0 + i) * kThreadsOfTeam;
-              if (task < tasks) q4::write_group<D>(tile, G::kPanel, task, x[i]);
-            }
-          }
+          decoder.run(packed, tile, keys);
           __syncwarp();
           if (lane == 0) mbar_arrive(bar_p_empty + 8 * s);
           clear_rest();

@@ -7,15 +7,14 @@
 // no atomics.  Per (key, query) the tensor pipe needs 2 D flops and the thread one fused multiply-add, an exponential and an addition.
 //
 // A step is a tile of 128 keys of a (layer, batch element, KV head) against 128 query rows; a tile meets all query rows of its KV head.
-// Block = 28 warps (20 without decoders), one block per SM with a contiguous share of the tiles:
-//   warps 0-15       sums of every other tile (two score buffers of 128 columns each), the first or second half of a step's columns: a warp's
-//                    chain of loads, multiply-adds, exponentials and additions is all latency, so four chains run beside each
-//                    other on each scheduler (28 layers at 16301 rows, bf16: 181 us with two)
-//   8 more           4-bit cache: decoders of K tiles, four warps for either group's
-//   then             producer (one lane): K tiles by TMA (bf16) or bulk copies (4 bits), query rows by TMA
-//   two              tcgen05.mma issuers for the two groups (one lane each)
-//   the last         the query rows' logarithms, and zeros for query rows that take no part
-// Query rows lie in two slots of 128: up to 256 stay there for all tiles of a unit, more go through for every pair of tiles.
+// Block = 32 warps (24 without decoders), one block per SM with a contiguous share of the tiles, dealt to four groups in turn.  What bounds a group
+// is latency: a tile takes it a chain of waits, decoding, products, loads from TMEM and sums of 2000 - 4000 cycles, hence four of them.
+//   warps 0-15       sums, four warps a group; a group has one K tile and 128 columns of TMEM (two score buffers of up to 64 query rows, else one)
+//   8 more           4-bit cache: decoders of K tiles, two warps for a group
+//   then             producer: K tiles by TMA (bf16) or bulk copies (4 bits), query rows by TMA
+//   four             tcgen05.mma issuers of the groups (one lane each)
+//   one              the query rows' logarithms, and zeros for query rows that take no part
+// Query rows lie in two slots of 128: up to 256 stay there for all tiles of a unit, more go through for every four tiles.
 #include <cuda_bf16.h>
 #include <math_constants.h>
 
@@ -35,20 +34,19 @@ constexpr int kMaxQCap = 4096;
 constexpr int kMaxGrid = 256;
 constexpr int kTmemCols = 512;
 constexpr int kBarrierBytes = 512, kFlagBytes = 64;
-constexpr int kSumWarps = 16;             // two halves of the columns for either group of tiles
+constexpr int kGroupsOfTiles = 4, kSumWarps = 4 * kGroupsOfTiles;
 
 template <int D, bool kQ4>
 struct Shape {
-  static constexpr int kDecodeWarps = kQ4 ? 8 : 0, kThreads = 32 * (kSumWarps + kDecodeWarps + 4);
+  static constexpr int kDecodeWarps = kQ4 ? 8 : 0, kThreads = 32 * (kSumWarps + kDecodeWarps + 8);
   static constexpr int kPanels = D / 64;
   static constexpr int kPanel = 128 * 128;           // bytes of a K tile's panel: 128 rows of 64 values
   static constexpr int kTile = kPanels * kPanel;
-  static constexpr int KS = 4;                       // K tiles, two for either group of warps
+  static constexpr int KS = kGroupsOfTiles;          // K tiles
   static constexpr int kPackedStage = q4::Packed<D, kKeys>::kBytes;
 };
 constexpr int kMaxPacked = 8;                        // packed K tiles: as many as there is room for
 constexpr int kLogBytes = 2 * kRows * 4;
-constexpr int kPartBytes = 2 * 4 * kKeys * 4;        // the second half's sums of a group's last four tiles
 
 struct Params {
   const int32_t* cache_len;
@@ -108,9 +106,8 @@ struct Ring {   // the next use of a ring of n stages: which stage, and the pari
   }
 };
 
-// Tiles begin, begin + 2, .. of a segment belong to group 0 of the warps, the others to group 1; tile i of a group (counted over the block's
-// life) has K stage 2 * group + (i & 1).  Every role enumerates the loads of query rows alike: events, event e in slot e & 1.  Up to two chunks:
-// one event each for a segment; more: one each for a pair of tiles.
+// Tiles begin + w, begin + w + 4, .. of a segment belong to group w of the warps.  Every role enumerates the loads of query rows alike: events,
+// event e in slot e & 1.  Up to two chunks: one event each for a segment; more: one each for four tiles.
 //
 // A wait for a barrier's phase works only when the phase before is over, so whoever waits on a barrier either has to arrive for its next
 // phase or waits behind something that does: hence stages that belong to one group, and events that each role takes, also where it has
@@ -125,9 +122,8 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_pad = (1024u - (smem_u32(smem_raw) & 1023u)) & 1023u;
   const uint32_t sm_k = smem_u32(smem_raw) + smem_pad, sm_q = sm_k + KS * G::kTile, sm_p = sm_q + 2 * q_slot;
-  const uint32_t sm_log = sm_p + (kQ4 ? PS * G::kPackedStage : 0), sm_part = sm_log + kLogBytes, sm_bar = sm_part + kPartBytes;
+  const uint32_t sm_log = sm_p + (kQ4 ? PS * G::kPackedStage : 0), sm_bar = sm_log + kLogBytes;
   float* const logs = reinterpret_cast<float*>(smem_raw + smem_pad + (sm_log - sm_k));
-  float* const parts = reinterpret_cast<float*>(smem_raw + smem_pad + (sm_part - sm_k));   // [group][tile & 3][key]
   int* const flags = reinterpret_cast<int*>(smem_raw + smem_pad + (sm_bar - sm_k) + kBarrierBytes);
   volatile int* const abort_ptr = flags;
   volatile int* const never_ptr = flags + 1;
@@ -136,31 +132,30 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 
   const uint32_t bar_k_full = sm_bar, bar_k_empty = bar_k_full + 8 * KS, bar_p_full = bar_k_empty + 8 * KS, bar_p_empty = bar_p_full + 8 * kMaxPacked;
   const uint32_t bar_q_tx = bar_p_empty + 8 * kMaxPacked, bar_q_ready = bar_q_tx + 16, bar_q_empty = bar_q_ready + 16;   // [slot]
-  const uint32_t bar_s_ready = bar_q_empty + 16, bar_s_empty = bar_s_ready + 32;                                // [warp group][buffer]
-  const uint32_t bar_drain = bar_s_empty + 32, bar_part = bar_drain + 16;                                       // [2], [group][tile & 3]
+  const uint32_t bar_s_ready = bar_q_empty + 16, bar_s_empty = bar_s_ready + 64, bar_drain = bar_s_empty + 64;   // [group][buffer], [group]
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     *abort_ptr = 0; *never_ptr = 0;
     for (int i = 0; i < KS; ++i) {
-      mbar_init(bar_k_full + 8 * i, kQ4 ? G::kDecodeWarps / 2 : 1);
+      mbar_init(bar_k_full + 8 * i, kQ4 ? G::kDecodeWarps / kGroupsOfTiles : 1);
       mbar_init(bar_k_empty + 8 * i, 1);
     }
     for (int i = 0; kQ4 && i < kMaxPacked; ++i) {
       mbar_init(bar_p_full + 8 * i, 1);
       mbar_init(bar_p_empty + 8 * i, G::kDecodeWarps);
     }
-    for (int i = 0; i < 8; ++i) mbar_init(bar_part + 8 * i, 4);
+
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar_q_tx + 8 * i, 1);
       mbar_init(bar_q_ready + 8 * i, 1);
-      mbar_init(bar_q_empty + 8 * i, kSumWarps + 2);   // and the issuers
-      mbar_init(bar_drain + 8 * i, 1);
+      mbar_init(bar_q_empty + 8 * i, kSumWarps + kGroupsOfTiles);   // and the issuers
     }
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2 * kGroupsOfTiles; ++i) {
       mbar_init(bar_s_ready + 8 * i, 1);
-      mbar_init(bar_s_empty + 8 * i, kSumWarps / 2);
+      mbar_init(bar_s_empty + 8 * i, 4);
     }
+    for (int i = 0; i < kGroupsOfTiles; ++i) mbar_init(bar_drain + 8 * i, 1);
     mbar_fence_init();
     fence_proxy_async_smem();
   }
@@ -182,6 +177,8 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   const uint32_t tmem = *tmem_slot;
   const Deal deal(len.prefix[p.batch], p.nl * p.n_kv_heads, (int)gridDim.x, 1);
   const bool resident = p.n_qc <= 2;
+  // score buffers of a group and their columns
+  const uint32_t n_buf = p.rows_total <= 64 ? 2 : 1, buf_cols = p.rows_total <= 64 ? 64 : 128;
   auto chunk_rows = [&](int c) { return min(kRows, p.rows_total - c * kRows); };
   Walk walk(p, len, deal, blockIdx.x);
   Segment g = {};
@@ -189,8 +186,9 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 
   if (warp == kControl) {
     // ================================================================= producer
-    uint32_t kt = 0, ev = 0, tiles[2] = {0, 0};   // packed tiles, events, tiles of the groups
+    uint32_t kt = 0, ev = 0;   // packed tiles and events so far; tiles of the groups (bf16)
     Ring ps;
+    uint32_t tiles[kGroupsOfTiles] = {};
     auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_warp(bar, parity, abort_ptr); };
     auto load_q = [&](int c) {
       const uint32_t s = ev & 1;
@@ -217,8 +215,8 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         ++kt;
         ps.advance(PS);
       } else {
-        const uint32_t i = tiles[w], s = 2 * w + (i & 1), bar = bar_k_full + 8 * s;
-        if (i >= 2 && !wait(bar_k_empty + 8 * s, ((i >> 1) - 1) & 1)) return false;
+        const uint32_t s = w, bar = bar_k_full + 8 * s;
+        if (tiles[w] > 0 && !wait(bar_k_empty + 8 * s, (tiles[w] - 1) & 1)) return false;
         if (lane == 0) mbar_expect_tx(bar, (uint32_t)p.k_box * 128u * G::kPanels);
         __syncwarp();
         if (lane < G::kPanels) tma_load_3d(sm_k + s * G::kTile + lane * G::kPanel, &tm_k, bar, lane * 64, t * kKeys, z);
@@ -230,9 +228,10 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     while (ok && walk.next(g)) {
       if (resident)
         for (int c = 0; c < p.n_qc && ok; ++c) ok = load_q(c);
-      for (int t = g.begin; t < g.end && ok; t += 2) {
-        ok = load_k(t, 0);
-        if (ok && t + 1 < g.end) ok = load_k(t + 1, 1);
+      for (int t = g.begin; t < g.end && ok; t += kGroupsOfTiles) {
+#pragma unroll
+        for (int w = 0; w < kGroupsOfTiles; ++w)
+          if (ok && t + w < g.end) ok = load_k(t + w, w);
         if (!resident)
           for (int c = 0; c < p.n_qc && ok; ++c) ok = load_q(c);
       }
@@ -241,11 +240,12 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     if (kQ4) {
       for (uint32_t i = kt > PS ? kt - PS : 0; i < kt; ++i) mbar_wait(bar_p_full + 8 * (i % PS), (i / PS) & 1, never_ptr);
     } else {
-      for (int w = 0; w < 2; ++w)
-        for (uint32_t i = tiles[w] > 2 ? tiles[w] - 2 : 0; i < tiles[w]; ++i) mbar_wait(bar_k_full + 8 * (2 * w + (i & 1)), (i >> 1) & 1, never_ptr);
+#pragma unroll
+      for (int w = 0; w < kGroupsOfTiles; ++w)
+        if (tiles[w] > 0) mbar_wait(bar_k_full + 8 * w, (tiles[w] - 1) & 1, never_ptr);
     }
     for (uint32_t i = ev > 2 ? ev - 2 : 0; i < ev; ++i) mbar_wait(bar_q_tx + 8 * (i & 1), (i >> 1) & 1, never_ptr);
-  } else if (warp == kControl + 1 || warp == kControl + 2) {
+  } else if (warp > kControl && warp <= kControl + kGroupsOfTiles) {
     if (elect_one_sync()) {
       // ================================================================= MMA issuers, one for each group of warps
       const int w = warp - kControl - 1;
@@ -254,21 +254,20 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       const uint64_t desc_k0 = make_smem_desc_sw128(sm_k, 16, 1024), desc_q0 = make_smem_desc_sw128(sm_q, 16, 1024);
       auto take_event = [&](uint32_t e) { return wait(bar_q_ready + 8 * (e & 1), (e >> 1) & 1); };
       while (ok && walk.next(g)) {
-        for (int t = g.begin + w; t - w < g.end && ok; t += 2) {
+        for (int t = g.begin + w; t - w < g.end && ok; t += kGroupsOfTiles) {
           const bool mine = t < g.end;
-          const uint32_t ks = 2 * w + (kt & 1);
-          if (mine) ok = wait(bar_k_full + 8 * ks, (kt >> 1) & 1);
+          if (mine) ok = wait(bar_k_full + 8 * w, kt & 1);
           for (int c = 0; c < p.n_qc && ok && (mine || !resident); ++c) {
             const uint32_t e = ev + c;
             ok = take_event(e);
             if (ok && mine) {
-              const uint32_t b = st & 1, buf = 16 * w + 8 * b;
-              ok = st < 2 || wait(bar_s_empty + buf, ((st >> 1) - 1) & 1);
+              const uint32_t b = st % n_buf, use = st / n_buf, buf = 16 * w + 8 * b;
+              ok = use == 0 || wait(bar_s_empty + buf, (use - 1) & 1);
               if (!ok) break;
               tc_fence_after_sync();
               const uint32_t idesc = make_idesc_bf16(128, (uint32_t)((chunk_rows(c) + 15) & ~15), 0);
-              const uint64_t dk = desc_offset(desc_k0, ks * G::kTile), dq = desc_offset(desc_q0, (e & 1) * q_slot);
-              const uint32_t d = tmem + w * 256 + b * kRows;
+              const uint64_t dk = desc_offset(desc_k0, w * G::kTile), dq = desc_offset(desc_q0, (e & 1) * q_slot);
+              const uint32_t d = tmem + w * 128 + b * buf_cols;
 #pragma unroll
               for (int k = 0; k < D / 16; ++k) {
                 const uint32_t a = ((k >> 2) * G::kPanel + (k & 3) * 32) >> 4, b_off = ((k >> 2) * p.q_panel + (k & 3) * 32) >> 4;
@@ -280,7 +279,7 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             if (ok && !resident) mbar_arrive(bar_q_empty + 8 * (e & 1));   // (the slot is not free before the group's warps have summed this step)
           }
           if (ok && mine) {
-            tc_commit(bar_k_empty + 8 * ks);
+            tc_commit(bar_k_empty + 8 * w);
             ++kt;
           }
           if (!resident) ev += p.n_qc;
@@ -296,11 +295,11 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       tc_commit(bar_drain + 8 * w);
       mbar_wait(bar_drain + 8 * w, 0, never_ptr);
     }
-  } else if (warp == kControl + 3) {
+  } else if (warp == kControl + kGroupsOfTiles + 1) {
     // ================================================================= query rows: logarithms, zeros
     uint32_t ev = 0;
     while (ok && walk.next(g)) {
-      const int events = resident ? p.n_qc : p.n_qc * ((g.end - g.begin + 1) / 2);
+      const int events = resident ? p.n_qc : p.n_qc * ((g.end - g.begin + kGroupsOfTiles - 1) / kGroupsOfTiles);
       const float* const lse = p.lse + (((size_t)g.layer * p.batch + g.b) * p.n_q_heads + (size_t)g.kvh * p.group) * p.q_cap;
       for (int i = 0, c = 0; i < events && ok; ++i, ++ev, c = c + 1 == p.n_qc ? 0 : c + 1) {
         const uint32_t s = ev & 1;
@@ -330,11 +329,12 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         if (lane == 0) mbar_arrive(bar_q_ready + 8 * s);
       }
     }
-  } else if (warp >= kSumWarps) {
+  } else if (warp >= kSumWarps && warp < kControl) {
     if constexpr (kQ4) {
-      // ================================================================= decoders, four warps for either group's tiles
-      constexpr int kTeam = G::kDecodeWarps / 2 * 32, kGroups = D / q4::kGroup, kPer = kKeys * kGroups / kTeam, kBatch = 2;
-      const int me = tid & (kTeam - 1), w = (warp - kSumWarps) / (G::kDecodeWarps / 2);
+      // ================================================================= decoders, two warps for a group's tiles
+      constexpr int kTeam = G::kDecodeWarps / kGroupsOfTiles * 32;
+      const q4::Decoder<D, kKeys, kTeam> decoder(tid & (kTeam - 1), G::kPanel);
+      const int w = (warp - kSumWarps) / (G::kDecodeWarps / kGroupsOfTiles);
       uint32_t n = 0;   // the group's tiles
       Ring ps;
       while (ok && walk.next(g)) {
@@ -342,71 +342,54 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           const uint32_t s = ps.stage, packed = sm_p + s * G::kPackedStage;
           ok = mbar_wait_warp(bar_p_full + 8 * s, ps.parity, abort_ptr);
           if (!ok) break;
-          if (((t - g.begin) & 1) != w) {
+          if (((t - g.begin) & (kGroupsOfTiles - 1)) != w) {
             __syncwarp();
             if (lane == 0) mbar_arrive(bar_p_empty + 8 * s);
             continue;
           }
-          const uint32_t ks = 2 * w + (n & 1), tile = sm_k + ks * G::kTile;
-          const int tasks = min(kKeys, g.Lc - t * kKeys) * kGroups;
-          if (n >= 2) ok = mbar_wait_warp(bar_k_empty + 8 * ks, ((n >> 1) - 1) & 1, abort_ptr);
+          const uint32_t tile = sm_k + w * G::kTile;
+          if (n > 0) ok = mbar_wait_warp(bar_k_empty + 8 * w, (n - 1) & 1, abort_ptr);
           if (!ok) break;
-          // (a short loop: unrolled, it and the sums' code drive each other out of the instruction caches)
-#pragma unroll 1
-          for (int i0 = 0; i0 < kPer; i0 += kBatch) {
-            q4::Group32 x[kBatch];
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-              const int task = me + (i0 + i) * kTeam;
-              if (task < tasks) x[i] = q4::read_group<D, kKeys>(packed, task);
-            }
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-              const int task = me + (i0 + i) * kTeam;
-              if (task < tasks) q4::write_group<D>(tile, G::kPanel, task, x[i]);
-            }
-          }
+          decoder.run(packed, tile, min(kKeys, g.Lc - t * kKeys));
           ++n;
           fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) {
             mbar_arrive(bar_p_empty + 8 * s);
-            mbar_arrive(bar_k_full + 8 * ks);
+            mbar_arrive(bar_k_full + 8 * w);
           }
         }
       }
     }
-  } else {
+  } else if (warp < kSumWarps) {
     // ================================================================= sums: thread = key of the tile = TMEM lane
-    const int w = warp >> 2 & 1, half = warp >> 3, key = (warp & 3) * 32 + lane;
-    const uint32_t t_s = tmem + ((uint32_t)((warp & 3) * 32) << 16) + w * 256;
+    const int w = warp >> 2, key = (warp & 3) * 32 + lane;
+    const uint32_t t_s = tmem + ((uint32_t)((warp & 3) * 32) << 16) + w * 128;
     const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2);
-    uint32_t ev = 0, st = 0, kt = 0;   // events, the group's steps and tiles
+    uint32_t ev = 0, st = 0;   // events, the group's steps
     while (ok && walk.next(g)) {
       const size_t row0 = (((size_t)(g.layer + p.layer_begin) * p.batch + g.b) * p.n_kv_heads + g.kvh) * p.capacity;
       // what the group's next tile has collected so far, asked for a tile ahead: a load from memory takes longer than a tile
       auto collected_of = [&](int t) {
         const int j = t * kKeys + key;
-        return half == 0 && t < g.end && j < g.Lc && p.collected && p.decay != 0.f ? p.collected[row0 + j] : 0.f;
+        return t < g.end && j < g.Lc && p.collected && p.decay != 0.f ? p.collected[row0 + j] : 0.f;
       };
       float ahead = collected_of(g.begin + w);
-      for (int t0 = g.begin; t0 < g.end && ok; t0 += 2) {
+      for (int t0 = g.begin; t0 < g.end && ok; t0 += kGroupsOfTiles) {
         const int t = t0 + w;
         if (t < g.end) {
-          float a0 = 0.f, a1 = 0.f, a2 = 0.f, a3 = 0.f;
+          uint64_t a01 = 0, a23 = 0;   // pairs of sums
           const int j = t * kKeys + key;
           const float before = ahead;
-          ahead = collected_of(t + 2);
+          ahead = collected_of(t + kGroupsOfTiles);
           for (int c = 0; c < p.n_qc && ok; ++c, ++st) {
-            const uint32_t e = ev + c, b = st & 1, buf = 16 * w + 8 * b;
+            const uint32_t e = ev + c, b = st % n_buf, use = st / n_buf, buf = 16 * w + 8 * b;
             const int n16 = (chunk_rows(c) + 15) & ~15;
-            ok = mbar_wait_warp(bar_s_ready + buf, (st >> 1) & 1, abort_ptr);   // (behind q_ready, whose logarithms are read here)
+            ok = mbar_wait_warp(bar_s_ready + buf, use & 1, abort_ptr);   // (behind q_ready, whose logarithms are read here)
             if (ok) ok = mbar_wait_warp(bar_q_ready + 8 * (e & 1), (e >> 1) & 1, abort_ptr);
             if (!ok) break;
             tc_fence_after_sync();
-            // this half's columns, 16 at a time
-            const int mid = ((n16 >> 4) + 1 >> 1) << 4, first = half ? mid : 0, last = half ? n16 : mid;
-            const uint32_t from = t_s + b * kRows, log_at = sm_log + (e & 1) * kRows * 4;
+            const uint32_t from = t_s + b * buf_cols, log_at = sm_log + (e & 1) * kRows * 4;
             auto add = [&](const uint32_t* v, int i0, int n) {
 #pragma unroll
               for (int i = 0; i < 32; i += 4) {
@@ -415,21 +398,19 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 float x0, x1, x2, x3;
                 unpack2(fma2(pack2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), scale2, pack2(l.x, l.y)), x0, x1);
                 unpack2(fma2(pack2(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])), scale2, pack2(l.z, l.w)), x2, x3);
-                a0 += ex2_approx(x0);
-                a1 += ex2_approx(x1);
-                a2 += ex2_approx(x2);
-                a3 += ex2_approx(x3);
+                a01 = add2(a01, pack2(ex2_approx(x0), ex2_approx(x1)));
+                a23 = add2(a23, pack2(ex2_approx(x2), ex2_approx(x3)));
               }
             };
             uint32_t v[32];
-            int i = first;
+            int i = 0;
 #pragma unroll 1
-            for (; i + 32 <= last; i += 32) {
+            for (; i + 32 <= n16; i += 32) {
               tmem_ld32(from + i, v);
               tmem_ld_wait();
               add(v, i, 32);
             }
-            if (i < last) {
+            if (i < n16) {
               tmem_ld16(from + i, v);
               tmem_ld_wait();
               add(v, i, 16);
@@ -442,21 +423,11 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             }
           }
           if (!ok) break;
-          // Four tiles' parts are kept: the second half is never that far ahead, since a score buffer waits for both halves, and the
-          // first half has read a tile's part before it releases a buffer of its next tile.
-          const float sum = (a0 + a1) + (a2 + a3);
-          float* const part = parts + (w * 4 + (kt & 3)) * kKeys + key;
-          const uint32_t bar = bar_part + (w * 4 + (kt & 3)) * 8;
-          if (half) {
-            *part = sum;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar);
-          } else {
-            ok = mbar_wait_warp(bar, (kt >> 2) & 1, abort_ptr);
-            if (ok && j < g.Lc) p.weight[row0 + j] = fmaf(p.decay, before, sum + *part);
-          }
-          ++kt;
-        } else if (!resident) {   // no second tile: the query rows are not needed here
+          float a0, a1, a2, a3;
+          unpack2(a01, a0, a1);
+          unpack2(a23, a2, a3);
+          if (j < g.Lc) p.weight[row0 + j] = fmaf(p.decay, before, (a0 + a1) + (a2 + a3));
+        } else if (!resident) {   // no tile for the group: the query rows are not needed here
           for (int c = 0; c < p.n_qc && ok; ++c) {
             ok = mbar_wait_warp(bar_q_ready + 8 * ((ev + c) & 1), ((ev + c) >> 1) & 1, abort_ptr);
             __syncwarp();
@@ -533,7 +504,7 @@ int accumulate(dlm_ctx* ctx, const Cache* cache, const uint8_t* k_scale, int lay
   p.q_panel = (uint32_t)((p.q_box + 15) & ~15) * 128u;
   const int tile = D == 128 ? Shape<128, kQ4>::kTile : Shape<64, kQ4>::kTile;
   const int packed = D == 128 ? Shape<128, kQ4>::kPackedStage : Shape<64, kQ4>::kPackedStage;
-  const int fixed = 1024 + Shape<128, kQ4>::KS * tile + 2 * (D / 64) * (int)p.q_panel + kLogBytes + kPartBytes + kBarrierBytes + kFlagBytes +
+  const int fixed = 1024 + Shape<128, kQ4>::KS * tile + 2 * (D / 64) * (int)p.q_panel + kLogBytes + kBarrierBytes + kFlagBytes +
                     4 * length_ints(cache->batch);
   p.n_packed = kQ4 ? (ctx->max_smem_optin - fixed) / packed : 0;
   if (p.n_packed > kMaxPacked) p.n_packed = kMaxPacked;

@@ -21,39 +21,57 @@ struct Packed {
   }
 };
 
-// One group of 32 values and its scale, taken from a packed tile: task i is group i % (D / 32) of row i / (D / 32), so that a warp reads
-// consecutive 16-byte pieces and consecutive bytes.
-struct Group32 {
-  uint32_t w[4];
-  uint32_t scale;
-};
-template <int D, int kRows>
-__device__ __forceinline__ Group32 read_group(uint32_t packed, int i) {
-  Group32 g;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(g.w[0]), "=r"(g.w[1]), "=r"(g.w[2]), "=r"(g.w[3]) : "r"(packed + i * 16) : "memory");
-  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(g.scale) : "r"(packed + Packed<D, kRows>::kData + i) : "memory");
-  return g;
-}
-
-// Decodes it into an operand tile: rows of 128 bytes (64 values) with 128-byte swizzle, a panel of 64 columns `panel_bytes` after the other.
-// Eight lanes have two rows of four groups (D = 128) or four rows of two: with the two panels' 16-byte pieces taken in another order
-// they store to eight different pieces of 128 bytes.
-template <int D>
-__device__ __forceinline__ void write_group(uint32_t tile, uint32_t panel_bytes, int i, const Group32& g) {
-  constexpr int kGroups = D / kGroup;
-  const int row = i / kGroups, grp = i % kGroups;
-  const uint32_t base = tile + (uint32_t)(grp >> 1) * panel_bytes + (uint32_t)row * 128u;
-  const Scale sc = make_scale(g.scale);
-  const int other = D == 128 ? (grp & 2) : 0;
-  const uint32_t w[4] = {other ? g.w[2] : g.w[0], other ? g.w[3] : g.w[1], other ? g.w[0] : g.w[2], other ? g.w[1] : g.w[3]};
+// Decodes a packed tile of kRows rows into an operand tile -- rows of 128 bytes (64 values) with 128-byte swizzle, a panel of 64 columns
+// `panel_bytes` after the other -- with a team of kTeam threads, a group of 32 values at a time.  Task i is group i % (D / 32) of row
+// i / (D / 32), so that a warp reads consecutive 16-byte pieces and consecutive bytes.  Eight lanes have two rows of four groups (D = 128) or four
+// rows of two: with the two panels' 16-byte pieces taken in another order they store to eight different pieces of 128 bytes.
+// A thread's tasks are a multiple of 8 rows apart, so all it needs to know of them is made once (Decoder) and a task takes about 62 instructions.
+template <int D, int kRows, int kTeam>
+struct Decoder {
+  static constexpr int kGroups = D / kGroup, kTasks = kRows * kGroups / kTeam;
+  static constexpr int kRowStep = kTeam / kGroups;          // rows between a thread's tasks
+  static_assert(kRowStep % 8 == 0 && kTeam % kGroups == 0 && (kRows * kGroups) % kTeam == 0, "tasks");
+  int row0, from16, from1;
+  uint32_t to[4];         // of the four pieces of a group, in the order of the words below
+  bool other;
+  __device__ __forceinline__ Decoder(int me, uint32_t panel_bytes) {
+    row0 = me / kGroups;
+    const int grp = me % kGroups;
+    from16 = me * 16;
+    from1 = Packed<D, kRows>::kData + me;
+    other = D == 128 && (grp & 2);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    uint32_t v[4];
-    decode8(w[j], sc, v);
-    const uint32_t piece = (uint32_t)((grp & 1) * 4 + (j ^ other)) ^ (uint32_t)(row & 7);
-    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + piece * 16u), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+    for (int j = 0; j < 4; ++j)
+      to[j] = (uint32_t)(grp >> 1) * panel_bytes + (uint32_t)row0 * 128u + (((uint32_t)((grp & 1) * 4 + (other ? j ^ 2 : j)) ^ (uint32_t)(row0 & 7)) << 4);
   }
-}
+  // rows of the tile from `rows` on are left as they are
+  __device__ __forceinline__ void run(uint32_t packed, uint32_t tile, int rows) const {
+    constexpr int kBatch = kTasks < 2 ? kTasks : 2;
+    // (a short loop: unrolled, it and the code of the other roles drive each other out of the instruction caches)
+#pragma unroll 1
+    for (int t = 0; t < kTasks; t += kBatch) {
+      uint32_t w[kBatch][4], b[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const uint32_t at = packed + (uint32_t)(t + i) * kTeam * 16u;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i][0]), "=r"(w[i][1]), "=r"(w[i][2]), "=r"(w[i][3]) : "r"(at + from16) : "memory");
+        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(b[i]) : "r"(packed + (uint32_t)(t + i) * kTeam + from1) : "memory");
+      }
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        if (row0 + (t + i) * kRowStep >= rows) continue;
+        const Scale sc = make_scale(b[i]);
+        const uint32_t base = tile + (uint32_t)((t + i) * kRowStep) * 128u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t v[4];
+          decode8(D == 128 && other ? w[i][j ^ 2] : w[i][j], sc, v);
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + to[j]), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+        }
+      }
+    }
+  }
+};
 
 // Clears 16-byte piece i of row i / (D / 8) of an operand tile.
 template <int D>
