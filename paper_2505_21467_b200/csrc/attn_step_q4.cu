@@ -5,15 +5,14 @@
 // bf16 tile that the products read holds it exactly; what is quantised is what was committed, nothing on the way.
 //
 // One unit is (layer, batch element, KV head, chunk of up to 256 query rows); its keys are taken in steps of 64, first the cache's,
-// then the fresh ones.  Block = 16 warps:
-//   warps 0-3    softmax of M tile 0 (128 query rows; thread = row = TMEM lane)
-//   warps 4-7    softmax of M tile 1, or with one M tile decoders like 8-11
-//   warps 8-11   decoders: packed K and V steps to bf16 operand tiles, a group of 32 values a thread at a time; two of their lanes
-//                have fresh rows copied straight into operand tiles (TMA)
-//   warp  12     producer (one lane): bulk copies of packed steps (a step's rows lie one after the other), TMA of Q
-//   warps 13, 14 tcgen05.mma issuers of M tile 0 / 1 (one lane each)
-// A step costs the tensor pipe about 1000 cycles with two M tiles, the softmax as much and the decoders 300 of each scheduler's issue
-// slots, so decoding is hidden; with one M tile it costs 500, and twice as many warps decode.
+// then the fresh ones.  Up to 32 query rows a KV head are a kernel of their own (attn_q4_few.cuh); above 128 a block has two M tiles of 128 query
+// rows that share every step, else one M tile, whose steps two chains of warps take in turn, each with an O, maxima and sums of its own that
+// are joined at the end.  What bounds a chain is latency (a step's softmax takes its warps 1800 cycles), so both forms have two.  Block = 16 or 20 warps:
+//   warps 0-3, 4-7   softmax of chain 0, 1 (thread = query row = TMEM lane)
+//   4 or 8 more      decoders: packed K and V steps to bf16 operand tiles, a group of 32 values a thread at a time; two or four of their lanes
+//                    have fresh rows copied straight into operand tiles (TMA)
+//   then             producer: bulk copies of packed steps (a step's rows lie one after the other), TMA of Q
+//   two              tcgen05.mma issuers of chain 0, 1 (one lane each)
 //
 // Every (unit, step) pair is one item of a global list and block c takes a contiguous share of it, at least `min_share` items: whole
 // units are finished by the block; a share's first and last unit may be a part, whose unnormalised O, maximum and sum go to the
@@ -29,32 +28,32 @@
 
 namespace {
 
-constexpr int kThreads = 512;
 constexpr int kStep = 64;                 // keys
 constexpr int kMaxBatch = 1024;
 constexpr int kMaxQCap = 4096;
 constexpr int kMaxGrid = 256;
 constexpr int kTmemCols = 512;
-constexpr int kRegsLaunch = 128;          // 512 threads: all of an SM's registers
-constexpr int kRegsSoftmax = 168, kRegsDecode = 104, kRegsControl = 72;
-static_assert(2 * kRegsSoftmax + kRegsDecode + kRegsControl <= 4 * kRegsLaunch, "register split of two M tiles");
-static_assert(kRegsSoftmax + 2 * kRegsDecode + kRegsControl <= 4 * kRegsLaunch, "register split of one M tile");
 constexpr int kBarrierBytes = 512, kFlagBytes = 64;
 
 template <int D, int NMT>
 struct Shape {
+  static constexpr bool kSplit = NMT == 1;                   // the chains share an M tile and split the steps
+  static constexpr int kDecodeWarps = kSplit ? 8 : 4, kTeamWarps = kDecodeWarps / 4, kControl = 8 + kDecodeWarps, kThreads = 32 * (kControl + 4);
+  // registers a thread: at launch all of the SM's, then by role
+  static constexpr int kRegsLaunch = kSplit ? 96 : 128, kRegsSoftmax = kSplit ? 136 : 168, kRegsDecode = kSplit ? 72 : 104, kRegsControl = kSplit ? 64 : 72;
+  static_assert(8 * kRegsSoftmax + kDecodeWarps * kRegsDecode + 4 * kRegsControl <= (kControl + 4) * kRegsLaunch, "register split");
   static constexpr int kPanels = D / 64;
   static constexpr int kQPanel = 128 * 128;                  // bytes: 128 rows of 64 values
   static constexpr int kQTile = kPanels * kQPanel;
   static constexpr int kPanel = kStep * 128;
   static constexpr int kTile = kPanels * kPanel;             // a step of K or V
   static constexpr int kPackedStage = 2 * q4::Packed<D, kStep>::kBytes;
-  static constexpr int KS = NMT == 2 ? 4 : 3, VS = 3;        // operand tiles
-  static constexpr int PS = NMT == 2 ? 4 : 8;                // packed steps in flight: with one M tile HBM is the bound
-  static constexpr int kDecodeWarps = NMT == 2 ? 4 : 8;
-  static constexpr int kTeamWarps = kDecodeWarps / 4;        // of the teams K even, K odd, V even, V odd
+  // Steps are dealt in turn to two lines (split: the chains), each with operand tiles, packed stages and decoders of its own
+  static constexpr int kDepthK = 2, kDepthV = kSplit ? 2 : 1, kDepthP = 3;
+  static constexpr int KS = 2 * kDepthK, VS = 2 * kDepthV, PS = 2 * kDepthP;
   static constexpr int kTiles = NMT * kQTile + (KS + VS) * kTile + PS * kPackedStage;
-  static constexpr uint32_t kColO = 0, kColS = 2 * D;        // O[mt] at mt * D, S[mt] at 2 D + mt * 128 (P in its place)
+  static constexpr int kFoldBytes = kSplit ? 2 * 128 * 8 : 0;   // (maximum, sum) of every row and chain
+  static constexpr uint32_t kColO = 0, kColS = 2 * D;        // O of chain c at c * D, its scores at 2 D + c * 128 (P in their place)
 };
 
 struct Params {
@@ -63,7 +62,7 @@ struct Params {
   const uint8_t *k, *v, *k_scale, *v_scale;
   __nv_bfloat16* out;
   float* lse;
-  float4* ws_o;     // [slot][D / 4][rows_pad]: a part's O, four columns of a row a vector
+  float4* ws_o;     // [slot][D / 4][rows_pad]: a part's O, four columns of a row a vector (few query rows: [slot][rows_pad][D / 4])
   float2* ws_ml;    // [slot][rows_pad]: its running maximum (log2 units) and sum
   int nl, layer_begin, batch, n_kv_heads, n_q_heads, group, capacity, q_cap;
   int rows_total;   // group * q_cap: query rows of a KV head
@@ -75,10 +74,13 @@ struct Params {
   int* status;
 };
 
-__device__ __forceinline__ int steps_of(int Lc, int Lq) { return Lq <= 0 ? 0 : (Lc + kStep - 1) / kStep + (Lq + kStep - 1) / kStep; }
+// Everything that counts steps is told their size: 64 keys, or 128 in the kernel for few query rows.
+template <int kKeys>
+__device__ __forceinline__ int steps_of(int Lc, int Lq) { return Lq <= 0 ? 0 : (Lc + kKeys - 1) / kKeys + (Lq + kKeys - 1) / kKeys; }
 
+template <int kKeys>
 __device__ __forceinline__ void read_lengths(const Params& p, const Lengths& s, volatile int* any_empty) {
-  read_lengths(p.cache_len, p.q_len, p.batch, p.capacity, p.q_cap, p.status, s, any_empty, steps_of);
+  read_lengths(p.cache_len, p.q_len, p.batch, p.capacity, p.q_cap, p.status, s, any_empty, steps_of<kKeys>);
 }
 __device__ __forceinline__ Deal deal_of(const Params& p, const Lengths& s, int grid) {
   return Deal(s.prefix[p.batch], p.nl * p.n_kv_heads * p.n_rc, grid, p.min_share);
@@ -93,6 +95,7 @@ struct Segment {
 };
 
 // The unit that an item belongs to (not its part).
+template <int kKeys>
 __device__ __forceinline__ void find_unit(const Params& p, const Lengths& s, const Deal& d, int item, Segment& g) {
   int rest;
   const int grp = d.group_of(item, rest);
@@ -100,11 +103,12 @@ __device__ __forceinline__ void find_unit(const Params& p, const Lengths& s, con
   g.layer = p.by_kv_heads.divmod(p.by_rc.divmod(grp, g.rc), g.kvh);
   g.Lc = s.lc[g.b];
   g.Lq = s.lq[g.b];
-  g.n_c = (g.Lc + kStep - 1) / kStep;
+  g.n_c = (g.Lc + kKeys - 1) / kKeys;
   g.unit_begin = grp * d.sum + s.prefix[g.b];
 }
 
 // Walks the segments of a block, alike in every role.
+template <int kKeys = kStep>
 struct Walk {
   const Params& p;
   const Lengths& s;
@@ -116,7 +120,7 @@ struct Walk {
   }
   __device__ __forceinline__ bool next(Segment& g) {
     if (at >= end) return false;
-    find_unit(p, s, d, at, g);
+    find_unit<kKeys>(p, s, d, at, g);
     const int steps = s.prefix[g.b + 1] - s.prefix[g.b];
     g.begin = at - g.unit_begin;
     g.end = min(steps, end - g.unit_begin);
@@ -126,23 +130,29 @@ struct Walk {
   }
 };
 
+template <int kKeys = kStep>
 __device__ __forceinline__ int step_keys(const Segment& g, int t) {
-  return t < g.n_c ? min(kStep, g.Lc - t * kStep) : min(kStep, g.Lq - (t - g.n_c) * kStep);
+  return t < g.n_c ? min(kKeys, g.Lc - t * kKeys) : min(kKeys, g.Lq - (t - g.n_c) * kKeys);
 }
 
+#include "attn_q4_few.cuh"
+
 template <int D, int NMT, bool kNoWait>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Shape<D, NMT>::kThreads, 1)
 q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_kn,
                     const __grid_constant__ CUtensorMap tm_vn, const __grid_constant__ Params p) {
   using G = Shape<D, NMT>;
   using Pk = q4::Packed<D, kStep>;
   constexpr uint64_t kLimit = kNoWait ? 0ull : kWaitLimitNs;
-  constexpr int KS = G::KS, VS = G::VS, PS = G::PS;
+  constexpr int KS = G::KS, VS = G::VS, PS = G::PS, kControl = G::kControl;
+  constexpr bool kSplit = G::kSplit;
+  constexpr int kStride = kSplit ? 2 : 1;   // of a chain's steps; its first is step c of a segment where they are split
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_pad = (1024u - (smem_u32(smem_raw) & 1023u)) & 1023u;
   const uint32_t sm_q = smem_u32(smem_raw) + smem_pad;
   const uint32_t sm_k = sm_q + NMT * G::kQTile, sm_v = sm_k + KS * G::kTile, sm_p = sm_v + VS * G::kTile, sm_bar = sm_p + PS * G::kPackedStage;
-  int* const flags = reinterpret_cast<int*>(smem_raw + smem_pad + G::kTiles + kBarrierBytes);
+  float2* const fold = reinterpret_cast<float2*>(smem_raw + smem_pad + G::kTiles + kBarrierBytes);   // [chain][row]
+  int* const flags = reinterpret_cast<int*>(smem_raw + smem_pad + G::kTiles + kBarrierBytes + G::kFoldBytes);
   volatile int* const abort_ptr = flags;        // raised by the first wait that gives up
   volatile int* const never_ptr = flags + 1;    // for waits that must not be cut short by an abort; raised by one that runs out
   uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(flags + 2);
@@ -152,20 +162,21 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   const uint32_t bar_q_full = sm_bar, bar_q_empty = sm_bar + 8, bar_drain = sm_bar + 16;              // drain [2]
   const uint32_t bar_s_ready = sm_bar + 32, bar_p_ready = sm_bar + 64, bar_pv_done = sm_bar + 96;     // [M tile][buffer]
   const uint32_t bar_k_full = sm_bar + 128, bar_k_empty = bar_k_full + 8 * KS, bar_v_full = bar_k_empty + 8 * KS, bar_v_empty = bar_v_full + 8 * VS;
-  const uint32_t bar_kf = bar_v_empty + 8 * VS, bar_vf = bar_kf + 8 * KS;                             // fresh rows copied
-  const uint32_t bar_p_full = bar_vf + 8 * VS, bar_p_empty = bar_p_full + 8 * PS;
-  static_assert(128 + 8 * (3 * KS + 3 * VS + 2 * PS) <= kBarrierBytes, "barriers");
+  const uint32_t bar_kf = bar_v_empty + 8 * VS, bar_vf = bar_kf + 16;                                 // [line]: fresh rows copied
+  const uint32_t bar_p_full = bar_vf + 16, bar_p_empty = bar_p_full + 8 * PS, bar_fold = bar_p_empty + 8 * PS;   // fold [2]
+  static_assert(128 + 8 * (2 * KS + 2 * VS + 4 + 2 * PS + 2) <= kBarrierBytes, "barriers");
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  // warps whose 32 query rows exist, of each M tile
-  auto live_warps = [&](int mt) { return (max(32, min(128, p.rows - 128 * mt)) + 31) / 32; };
+  // warps whose 32 query rows exist, of each chain
+  auto live_warps = [&](int c) { return (max(32, min(128, p.rows - (kSplit ? 0 : 128 * c))) + 31) / 32; };
 
   if (tid == 0) {
     *abort_ptr = 0; *never_ptr = 0; *any_empty = 0;
     mbar_init(bar_q_full, 1);
-    mbar_init(bar_q_empty, NMT);
+    mbar_init(bar_q_empty, 2);
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar_drain + 8 * i, 1);
+      mbar_init(bar_fold + 8 * i, (uint32_t)(2 * live_warps(0)));
       for (int u = 0; u < 2; ++u) {
         mbar_init(bar_s_ready + 16 * i + 8 * u, 1);
         mbar_init(bar_p_ready + 16 * i + 8 * u, (uint32_t)live_warps(i));
@@ -173,47 +184,49 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       }
     }
     for (int i = 0; i < KS; ++i) {
-      mbar_init(bar_k_full + 8 * i, 2 * G::kTeamWarps);
+      mbar_init(bar_k_full + 8 * i, G::kTeamWarps);
       mbar_init(bar_k_empty + 8 * i, NMT);
-      mbar_init(bar_kf + 8 * i, 1);
     }
     for (int i = 0; i < VS; ++i) {
-      mbar_init(bar_v_full + 8 * i, 2 * G::kTeamWarps);
+      mbar_init(bar_v_full + 8 * i, G::kTeamWarps);
       mbar_init(bar_v_empty + 8 * i, NMT);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar_kf + 8 * i, 1);
       mbar_init(bar_vf + 8 * i, 1);
     }
     for (int i = 0; i < PS; ++i) {
       mbar_init(bar_p_full + 8 * i, 1);
-      mbar_init(bar_p_empty + 8 * i, 2 * G::kTeamWarps);
+      mbar_init(bar_p_empty + 8 * i, 2 * G::kTeamWarps);   // K and V
     }
     mbar_fence_init();
     fence_proxy_async_smem();
   }
-  if (warp == 13) {
+  if (warp == kControl + 1) {
     tmem_alloc(smem_u32(tmem_slot), kTmemCols);
     tmem_relinquish();
   }
-  if (warp == 12 && lane == 0) {
+  if (warp == kControl && lane == 0) {
     prefetch_tensormap(&tm_q);
     prefetch_tensormap(&tm_kn);
     prefetch_tensormap(&tm_vn);
   }
   dlm_grid_dependency_wait();
   dlm_trigger_dependents();
-  if (warp == 0) read_lengths(p, len, any_empty);
+  if (warp == 0) read_lengths<kStep>(p, len, any_empty);
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = *tmem_slot;
   const Deal deal = deal_of(p, len, (int)gridDim.x);
 
-  if (warp >= 12) {
-    setmaxnreg_dec<kRegsControl>();
-    if (warp == 12) {
+  if (warp >= kControl) {
+    setmaxnreg_dec<G::kRegsControl>();
+    if (warp == kControl) {
       // ================================================================= producer
-      Walk walk(p, len, deal, blockIdx.x);
+      Walk<> walk(p, len, deal, blockIdx.x);
       Segment g = {};
-      uint32_t ps = 0, n_q = 0;   // packed steps and Q tiles so far
+      uint32_t st = 0, n_q = 0, copied[2] = {0, 0};   // steps, Q tiles, packed steps of the lines so far
       bool ok = true, q_due = false;
       auto issue_q = [&]() {
         q_due = false;
@@ -236,9 +249,10 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         q_due = true;
         if (n_q == 0) ok = issue_q();
         const size_t head = ((size_t)(g.layer + p.layer_begin) * p.batch + g.b) * p.n_kv_heads + g.kvh;
-        for (int t = g.begin; t < min(g.end, g.n_c) && ok; ++t, ++ps) {
-          const uint32_t s = ps % PS, bar = bar_p_full + 8 * s;
-          if (ps >= (uint32_t)PS) ok = wait(bar_p_empty + 8 * s, (ps / PS - 1) & 1);
+        for (int t = g.begin; t < min(g.end, g.n_c) && ok; ++t) {
+          const uint32_t i = t - g.begin, x = (kSplit ? i : st + i) & 1, n = x ? copied[1] : copied[0];
+          const uint32_t s = x * G::kDepthP + n % G::kDepthP, bar = bar_p_full + 8 * s;
+          if (n >= (uint32_t)G::kDepthP) ok = wait(bar_p_empty + 8 * s, (n / G::kDepthP - 1) & 1);
           if (!ok) break;
           const int rows = step_keys(g, t);
           if (lane == 0) mbar_expect_tx(bar, 2 * Pk::bytes(rows));
@@ -247,34 +261,45 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             Pk::copy_part(sm_p + s * G::kPackedStage + (lane >> 1) * Pk::kBytes, lane < 2 ? p.k : p.v, lane < 2 ? p.k_scale : p.v_scale, lane & 1,
                           head * p.capacity + (size_t)t * kStep, rows, bar);
           __syncwarp();
+          if (x) ++copied[1]; else ++copied[0];
         }
+        st += g.end - g.begin;
         if (ok && q_due) ok = issue_q();
       }
       // no copy lands after the block has released its shared memory
-      for (uint32_t i = ps > (uint32_t)PS ? ps - PS : 0; i < ps; ++i) mbar_wait(bar_p_full + 8 * (i % PS), (i / PS) & 1, never_ptr);
+      for (uint32_t x = 0; x < 2; ++x) {
+        const uint32_t n = x ? copied[1] : copied[0];
+        for (uint32_t i = n > (uint32_t)G::kDepthP ? n - G::kDepthP : 0; i < n; ++i)
+          mbar_wait(bar_p_full + 8 * (x * G::kDepthP + i % G::kDepthP), (i / G::kDepthP) & 1, never_ptr);
+      }
       if (n_q > 0) mbar_wait(bar_q_full, (n_q - 1) & 1, never_ptr);
-    } else if ((warp == 13 || warp == 14) && warp - 13 < NMT && elect_one_sync()) {
+    } else if ((warp == kControl + 1 || warp == kControl + 2) && elect_one_sync()) {
       // ================================================================= MMA issuers, one lane each
-      const int mt = warp - 13;
+      const int c = warp - kControl - 1;
       auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_limit(bar, parity, abort_ptr, kLimit); };
-      Walk walk(p, len, deal, blockIdx.x);
+      Walk<> walk(p, len, deal, blockIdx.x);
       Segment g = {};
-      uint32_t st = 0, pt = 0, seg = 0;   // steps whose scores / whose P V product have been issued
+      uint32_t st = 0, pt = 0, seg = 0;   // the chain's steps whose scores / whose P V product have been issued
       bool ok = true;
       const uint32_t idesc_pv = make_idesc_bf16(128, D, 1);
-      const uint64_t desc_q = make_smem_desc_sw128(sm_q + mt * G::kQTile, 16, 1024);
+      const uint64_t desc_q = make_smem_desc_sw128(sm_q + (kSplit ? 0 : c) * G::kQTile, 16, 1024);
       const uint64_t desc_k0 = make_smem_desc_sw128(sm_k, 16, 1024);
       const uint64_t desc_v0 = make_smem_desc_sw128(sm_v, G::kPanel, 1024);
-      const uint32_t t_o = tmem + G::kColO + mt * D, t_s = tmem + G::kColS + mt * 128;
+      const uint32_t t_o = tmem + G::kColO + c * D, t_s = tmem + G::kColS + c * 128;
+      // operand tile of the chain's n-th step, and the use of it that this is
+      auto stage = [&](uint32_t n, uint32_t ring) { return kSplit ? 2 * c + (n & 1) : n % ring; };
+      auto use = [&](uint32_t n, uint32_t ring) { return kSplit ? n >> 1 : n / ring; };
       while (ok && walk.next(g)) {
         ok = wait(bar_q_full, seg & 1);
         if (!ok) break;
-        int ts = g.begin;
+        const int first = g.begin + (kSplit ? c : 0);
+        int ts = first;
+        if (ts >= g.end) mbar_arrive(bar_q_empty);   // no step of the segment for this chain
         // scores of the next step that has none yet, into buffer st & 1
         auto issue_s = [&]() -> bool {
           if (ts >= g.end) return true;
-          const uint32_t ks = st % KS;
-          if (!wait(bar_k_full + 8 * ks, (st / KS) & 1)) return false;
+          const uint32_t ks = stage(st, KS);
+          if (!wait(bar_k_full + 8 * ks, use(st, KS) & 1)) return false;
           tc_fence_after_sync();
           const uint32_t idesc = make_idesc_bf16(128, (uint32_t)((step_keys(g, ts) + 15) & ~15), 0);
           const uint64_t dk = desc_offset(desc_k0, ks * G::kTile);
@@ -284,125 +309,110 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             const uint32_t a = ((k >> 2) * G::kQPanel + (k & 3) * 32) >> 4, b = ((k >> 2) * G::kPanel + (k & 3) * 32) >> 4;
             mma_ss_lo<false>(d, (uint32_t)desc_q + a, (uint32_t)dk + b, (uint32_t)(desc_q >> 32), idesc, k > 0 ? 1u : 0u);
           }
-          tc_commit(bar_s_ready + 16 * mt + 8 * (st & 1));
+          tc_commit(bar_s_ready + 16 * c + 8 * (st & 1));
           tc_commit(bar_k_empty + 8 * ks);
           ++st;
-          if (++ts >= g.end) tc_commit(bar_q_empty);   // Q is not read again in this segment
+          ts += kStride;
+          if (ts >= g.end) tc_commit(bar_q_empty);   // Q is not read again in this segment
           return true;
         };
         ok = issue_s() && issue_s();
-        for (int t = g.begin; t < g.end && ok; ++t, ++pt) {
-          const uint32_t vs = pt % VS, buf = pt & 1;
-          ok = wait(bar_v_full + 8 * vs, (pt / VS) & 1) && wait(bar_p_ready + 16 * mt + 8 * buf, (pt >> 1) & 1);
+        for (int t = first; t < g.end && ok; t += kStride, ++pt) {
+          const uint32_t vs = stage(pt, VS), buf = pt & 1;
+          ok = wait(bar_v_full + 8 * vs, use(pt, VS) & 1) && wait(bar_p_ready + 16 * c + 8 * buf, (pt >> 1) & 1);
           if (!ok) break;
           tc_fence_after_sync();
           const int n16 = (step_keys(g, t) + 15) & ~15;
           const uint64_t dv = desc_offset(desc_v0, vs * G::kTile);
           const uint32_t a = t_s + buf * kStep;
-          if (t == g.begin) mma_ts<false>(t_o, a, dv, idesc_pv); else mma_ts<true>(t_o, a, dv, idesc_pv);
+          if (t == first) mma_ts<false>(t_o, a, dv, idesc_pv); else mma_ts<true>(t_o, a, dv, idesc_pv);
           if (n16 == kStep) {
 #pragma unroll
             for (int i = 1; i < kStep / 16; ++i) mma_ts<true>(t_o, a + i * 8, desc_offset(dv, i * 2048), idesc_pv);
           } else {
             for (int i = 1; i < n16 / 16; ++i) mma_ts<true>(t_o, a + i * 8, desc_offset(dv, i * 2048), idesc_pv);
           }
-          tc_commit(bar_pv_done + 16 * mt + 8 * buf);
+          tc_commit(bar_pv_done + 16 * c + 8 * buf);
           tc_commit(bar_v_empty + 8 * vs);
           ok = issue_s();   // the buffer just consumed takes the step after next
         }
         ++seg;
       }
       // every MMA issued by this lane has finished before TMEM and shared memory are released
-      tc_commit(bar_drain + 8 * mt);
-      mbar_wait(bar_drain + 8 * mt, 0, never_ptr);
+      tc_commit(bar_drain + 8 * c);
+      mbar_wait(bar_drain + 8 * c, 0, never_ptr);
     }
-  } else if (warp >= 8 || (NMT == 1 && warp >= 4)) {
-    // ================================================================= decoders
-    // Four teams: K or V tiles, of the even or of the odd packed steps.  A tile costs a warp a chain of waits, loads, conversions, stores, a
-    // fence and an arrival, most of it latency: with all warps on the same tile, K then V, a step took 1900 cycles; so the chains of
-    // two steps and of K and V run beside each other.  Every team waits for every stage of its kind to be free and arrives for it, also where it has
-    // nothing to store, so that its arrivals cannot run ahead into the stage's next phase.
-    setmaxnreg_dec<kRegsDecode>();
-    static_assert(PS % 2 == 0, "a packed stage belongs to one pair of teams");
+  } else if (warp >= 8) {
+    // ================================================================= decoders: K of line 0, K of line 1, V of line 0, V of line 1
+    // (a tile costs a warp a chain of waits, loads, conversions, stores, a fence and an arrival, most of it latency: the teams' run side by
+    // side, and what a team waits on is its own, so that it need not follow the others' steps)
+    setmaxnreg_dec<G::kRegsDecode>();
     constexpr int kThreadsOfTeam = G::kTeamWarps * 32;
-    const int w = warp - (kThreads / 32 - 4 - G::kDecodeWarps), team = w / G::kTeamWarps, me = tid & (kThreadsOfTeam - 1);
-    const bool is_k = team < 2, asks = (team & 1) == 0 && me == 0;
-    const uint32_t odd = team & 1, stages = is_k ? KS : VS, tiles = is_k ? sm_k : sm_v, part = is_k ? 0 : Pk::kBytes;
-    const uint32_t bar_full = is_k ? bar_k_full : bar_v_full, bar_empty = is_k ? bar_k_empty : bar_v_empty, bar_fresh = is_k ? bar_kf : bar_vf;
+    const int team = (warp - 8) / G::kTeamWarps, me = tid & (kThreadsOfTeam - 1);
+    const bool is_k = team < 2;
+    const uint32_t x = team & 1, depth = is_k ? G::kDepthK : G::kDepthV, part = is_k ? 0 : Pk::kBytes, packed0 = sm_p + x * G::kDepthP * G::kPackedStage;
+    // operand tile i of the line: split, the line's tiles lie together; else the lines' alternate
+    const uint32_t first_tile = kSplit ? x * depth : x, tile_step = kSplit ? 1 : 2;
+    const uint32_t tiles = (is_k ? sm_k : sm_v) + first_tile * G::kTile;
+    const uint32_t bar_full = (is_k ? bar_k_full : bar_v_full) + 8 * first_tile, bar_empty = (is_k ? bar_k_empty : bar_v_empty) + 8 * first_tile;
+    const uint32_t bar_fresh = (is_k ? bar_kf : bar_vf) + 8 * x, bar_packed = bar_p_full + 8 * x * G::kDepthP, bar_read = bar_p_empty + 8 * x * G::kDepthP;
     const q4::Decoder<D, kStep, kThreadsOfTeam> decoder(me, G::kPanel);
     auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_warp(bar, parity, abort_ptr, kLimit); };
-    Walk walk(p, len, deal, blockIdx.x);
+    Walk<> walk(p, len, deal, blockIdx.x);
     Segment g = {};
-    uint32_t st = 0, ps = 0, fs = 0, asked = 0;   // steps, packed and fresh ones so far; fresh tiles asked for (by one lane)
-    bool ok = true;
+    uint32_t st = 0, n = 0, ps = 0, fs = 0;   // steps; the line's steps, packed ones and fresh ones
+    bool ok = true, asked = false;
     while (ok && walk.next(g)) {
-      int t_ask = max(g.n_c, g.begin);   // the fresh step whose tile is asked for next
-      for (int t = g.begin; t < g.end && ok; ++t, ++st) {
-        // One lane of the K teams and one of the V teams copy the fresh rows, as far ahead as there are tiles free: for the step at hand they
-        // wait for that, for later ones they only look.  (Not the producer: it runs further ahead of the products than a
-        // stage's barrier can tell, since a wait for a phase works only when the one before it is over.)
-        if (asks) {
-          for (; t_ask < g.end && t_ask - t < (int)stages; ++t_ask, ++asked) {
-            const uint32_t i = st + (t_ask - t), s = i % stages, bar = bar_fresh + 8 * (asked % stages), parity = (i / stages - 1) & 1;
-            if (i >= stages && !(t_ask == t ? mbar_wait_limit(bar_empty + 8 * s, parity, abort_ptr, kLimit) : mbar_test_wait(bar_empty + 8 * s, parity))) break;
-            mbar_expect_tx(bar, (uint32_t)p.fresh_box * 128u * G::kPanels);
-            for (int pn = 0; pn < G::kPanels; ++pn)
-              tma_load_3d(tiles + s * G::kTile + pn * G::kPanel, is_k ? &tm_kn : &tm_vn, bar, pn * 64, (t_ask - g.n_c) * kStep,
-                          (g.layer * p.batch + g.b) * p.n_kv_heads + g.kvh);
-          }
-        }
-        __syncwarp();
-        const uint32_t stage = st % stages, tile = tiles + stage * G::kTile;
+      for (int t = g.begin + (int)((kSplit ? x : x ^ st) & 1); t < g.end && ok; t += 2, ++n) {
+        const uint32_t i = tile_step * (depth == 2 ? n & 1 : 0), use = depth == 2 ? n >> 1 : n, tile = tiles + i * G::kTile;
         const int keys = step_keys(g, t), n16 = (keys + 15) & ~15;
-        // V rows from `keys` to the next multiple of 16 meet P = 0: clear them, so that a NaN left there cannot reach O
-        auto clear_rest = [&]() {
-          if (!is_k)
-            for (int i = keys * (D / 8) + me; i < n16 * (D / 8); i += kThreadsOfTeam) q4::clear_piece<D>(tile, G::kPanel, i);
-        };
-        const bool fresh = t >= g.n_c, mine = !fresh && (ps++ & 1) == odd;
-        if (!mine && st >= stages) {
-          ok = wait(bar_empty + 8 * stage, (st / stages - 1) & 1);
+        if (use > 0) ok = wait(bar_empty + 8 * i, (use - 1) & 1);
+        if (!ok) break;
+        if (t < g.n_c) {
+          const uint32_t q = ps % G::kDepthP;
+          ok = wait(bar_packed + 8 * q, (ps / G::kDepthP) & 1);
           if (!ok) break;
-        }
-        if (fresh) {
-          ok = wait(bar_fresh + 8 * (fs % stages), (fs / stages) & 1);
-          if (!ok) break;
-          ++fs;
-          if (odd == 0) clear_rest();
-        } else if (mine) {
-          const uint32_t s = (ps - 1) % PS, packed = sm_p + s * G::kPackedStage + part;
-          ok = wait(bar_p_full + 8 * s, ((ps - 1) / PS) & 1);
-          if (!ok) break;
-          if (st >= stages) {
-            ok = wait(bar_empty + 8 * stage, (st / stages - 1) & 1);
-            if (!ok) break;
-          }
-          decoder.run(packed, tile, keys);
+          decoder.run(packed0 + q * G::kPackedStage + part, tile, keys);
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar_p_empty + 8 * s);
-          clear_rest();
+          if (lane == 0) mbar_arrive(bar_read + 8 * q);
+          ++ps;
+        } else {
+          if (me == 0) {
+            mbar_expect_tx(bar_fresh, (uint32_t)p.fresh_box * 128u * G::kPanels);
+            for (int pn = 0; pn < G::kPanels; ++pn)
+              tma_load_3d(tile + pn * G::kPanel, is_k ? &tm_kn : &tm_vn, bar_fresh, pn * 64, (t - g.n_c) * kStep, (g.layer * p.batch + g.b) * p.n_kv_heads + g.kvh);
+          }
+          asked = true;
+          __syncwarp();
+          ok = wait(bar_fresh, fs & 1);
+          if (!ok) break;
+          asked = false;
+          ++fs;
         }
+        // V rows from `keys` to the next multiple of 16 meet P = 0: clear them, so that a NaN left there cannot reach O
+        if (!is_k)
+          for (int j = keys * (D / 8) + me; j < n16 * (D / 8); j += kThreadsOfTeam) q4::clear_piece<D>(tile, G::kPanel, j);
         // what was stored to the tile is visible to the tensor cores before it is announced
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar_full + 8 * stage);
+        if (lane == 0) mbar_arrive(bar_full + 8 * i);
       }
+      st += g.end - g.begin;
     }
-    // no copy lands after the block has released its shared memory (here and in the producer: they have landed long since unless the
-    // block is unwinding)
-    for (uint32_t i = asked > stages ? asked - stages : 0; i < asked; ++i) mbar_wait(bar_fresh + 8 * (i % stages), (i / stages) & 1, never_ptr);
+    // a copy that was given up lands before the block has released its shared memory
+    if (asked && me == 0) mbar_wait(bar_fresh, fs & 1, never_ptr);
   } else {
     // ================================================================= softmax warps (those that own real rows)
-    setmaxnreg_inc<kRegsSoftmax>();
-    const int mt = warp >> 2, row = (warp & 3) * 32 + lane, r_unit = mt * 128 + row;
-    if ((warp & 3) < live_warps(mt)) {
+    setmaxnreg_inc<G::kRegsSoftmax>();
+    const int c = warp >> 2, row = (warp & 3) * 32 + lane, r_unit = kSplit ? row : c * 128 + row;
+    if ((warp & 3) < live_warps(c)) {
       const uint32_t t_lane = (uint32_t)((warp & 3) * 32) << 16;
-      const uint32_t t_s = tmem + t_lane + G::kColS + mt * 128, t_o = tmem + t_lane + G::kColO + mt * D;
+      const uint32_t t_s = tmem + t_lane + G::kColS + c * 128, t_o = tmem + t_lane + G::kColO + c * D;
       auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_warp(bar, parity, abort_ptr, kLimit); };
       auto out_row = [&](int layer, int b, int kvh, int rc) {
         return (((size_t)layer * p.batch + b) * p.n_q_heads + (size_t)kvh * p.group) * p.q_cap + rc * p.chunk + r_unit;
       };
-      if (*any_empty) {
+      if (*any_empty && (!kSplit || c == 0)) {
         // units without any key (inactive batch elements) appear in no share: their rows are zero
         const int n_units = p.nl * p.n_kv_heads * p.n_rc * p.batch;
         for (int unit = blockIdx.x; unit < n_units; unit += gridDim.x) {
@@ -411,49 +421,82 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           if (len.prefix[b + 1] != len.prefix[b] || r_unit >= p.rows || rc * p.chunk + r_unit >= p.rows_total) continue;
           const size_t r = out_row(layer, b, kvh, rc);
 #pragma unroll
-          for (int c = 0; c < D / 8; ++c) reinterpret_cast<uint4*>(p.out + r * D)[c] = make_uint4(0, 0, 0, 0);
+          for (int i = 0; i < D / 8; ++i) reinterpret_cast<uint4*>(p.out + r * D)[i] = make_uint4(0, 0, 0, 0);
           if (p.lse) p.lse[r] = -CUDART_INF_F;
         }
       }
-      Walk walk(p, len, deal, blockIdx.x);
+      Walk<> walk(p, len, deal, blockIdx.x);
       Segment g = {};
-      uint32_t st = 0;
+      uint32_t st = 0, seg = 0;   // the chain's steps; segments
       bool ok = true;
       while (ok && walk.next(g)) {
         float m_used = -CUDART_INF_F, l_run = 0.f;
         const int r_kv = g.rc * p.chunk + r_unit;
         const bool real = r_unit < p.rows && r_kv < p.rows_total, active = real && r_kv - p.by_q_cap.div(r_kv) * p.q_cap < g.Lq;
-        for (int t = g.begin; t < g.end; ++t, ++st) {
-          const uint32_t buf = st & 1, before = 16 * mt + 8 * ((st - 1) & 1), parity = ((st - 1) >> 1) & 1;
-          ok = wait(bar_s_ready + 16 * mt + 8 * buf, (st >> 1) & 1);
+        const int first = g.begin + (kSplit ? c : 0);
+        for (int t = first; t < g.end; t += kStride, ++st) {
+          const uint32_t buf = st & 1, before = 16 * c + 8 * ((st - 1) & 1), parity = ((st - 1) >> 1) & 1;
+          ok = wait(bar_s_ready + 16 * c + 8 * buf, (st >> 1) & 1);
           if (!ok) break;
           tc_fence_after_sync();
           const int keys = step_keys(g, t);
           if (keys == kStep)
-            ok = softmax_half_full<D>(t_s + buf * kStep, t_o, t == g.begin, p.scale_log2, m_used, l_run, bar_pv_done + before, parity, abort_ptr, active);
+            ok = softmax_half_full<D>(t_s + buf * kStep, t_o, t == first, p.scale_log2, m_used, l_run, bar_pv_done + before, parity, abort_ptr, active);
           else
-            ok = softmax_half_ragged<D>(t_s + buf * kStep, t_o, keys, t == g.begin, p.scale_log2, m_used, l_run, bar_pv_done + before, parity, abort_ptr, active);
+            ok = softmax_half_ragged<D>(t_s + buf * kStep, t_o, keys, t == first, p.scale_log2, m_used, l_run, bar_pv_done + before, parity, abort_ptr, active);
           if (!ok) break;
           __syncwarp();
           if (lane == 0) {
             tc_fence_before_sync();
-            mbar_arrive(bar_p_ready + 16 * mt + 8 * buf);
+            mbar_arrive(bar_p_ready + 16 * c + 8 * buf);
           }
         }
         // ---- O is complete once the last P V product has finished
-        if (ok) ok = wait(bar_pv_done + 16 * mt + 8 * ((st - 1) & 1), ((st - 1) >> 1) & 1);
+        if (ok && first < g.end) ok = wait(bar_pv_done + 16 * c + 8 * ((st - 1) & 1), ((st - 1) >> 1) & 1);
         if (!ok) break;
         tc_fence_after_sync();
+        // split: both chains' threads of a row learn of each other's maximum and sum, then each has half of the columns
+        float w0 = 1.f, w1 = 0.f;
+        bool both = false;
+        if (kSplit) {
+          fold[c * 128 + row] = make_float2(m_used, l_run);
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar_fold);
+          ok = wait(bar_fold, seg & 1);
+          if (!ok) break;
+          tc_fence_after_sync();
+          const float2 a = fold[row], b = fold[128 + row];
+          both = g.end - g.begin > 1;
+          m_used = both ? fmaxf(a.x, b.x) : a.x;
+          w0 = both ? ex2_approx(a.x - m_used) : 1.f;
+          w1 = both ? ex2_approx(b.x - m_used) : 0.f;
+          l_run = both ? fmaf(w0, a.y, w1 * b.y) : a.y;
+        }
+        constexpr int kCols = kSplit ? D / 2 : D;   // that this thread joins and stores, from c0 on
+        const int c0 = kSplit ? c * kCols : 0;
+        const uint32_t t_first = kSplit ? t_o - c * D : t_o;
         uint32_t v[32];
+        auto read_o = [&](int col) {
+          tmem_ld32(t_first + col, v);
+          if (kSplit && both) {
+            uint32_t u[32];
+            tmem_ld32(t_first + D + col, u);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(fmaf(w1, __uint_as_float(u[j]), w0 * __uint_as_float(v[j])));
+          } else {
+            tmem_ld_wait();
+          }
+        };
         if (g.slot < 0) {
           const float inv = active ? 1.f / l_run : 0.f;
           const size_t r = out_row(g.layer, g.b, g.kvh, g.rc);
 #pragma unroll 1
-          for (int c = 0; c < D / 32; ++c) {
-            tmem_ld32(t_o + c * 32, v);
-            tmem_ld_wait();
+          for (int col = c0; col < c0 + kCols; col += 32) {
+            read_o(col);
             if (!real) continue;
-            uint4* o = reinterpret_cast<uint4*>(p.out + r * D + c * 32);
+            uint4* o = reinterpret_cast<uint4*>(p.out + r * D + col);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               uint32_t h[4];
@@ -463,21 +506,26 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
               o[i] = make_uint4(h[0], h[1], h[2], h[3]);
             }
           }
-          if (real && p.lse) p.lse[r] = active ? (m_used + lg2_approx(l_run)) * 0.6931471805599453f : -CUDART_INF_F;
+          if (real && p.lse && c0 == 0) p.lse[r] = active ? (m_used + lg2_approx(l_run)) * 0.6931471805599453f : -CUDART_INF_F;
         } else {
           float4* po = p.ws_o + (size_t)g.slot * (D / 4) * p.rows_pad + r_unit;
 #pragma unroll 1
-          for (int c = 0; c < D / 32; ++c) {
-            tmem_ld32(t_o + c * 32, v);
-            tmem_ld_wait();
+          for (int col = c0; col < c0 + kCols; col += 32) {
+            read_o(col);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-              __stcg(po + (size_t)(c * 8 + j) * p.rows_pad, make_float4(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1]),
-                                                                        __uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3])));
+              __stcg(po + (size_t)(col / 4 + j) * p.rows_pad, make_float4(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1]),
+                                                                          __uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3])));
           }
-          __stcg(p.ws_ml + (size_t)g.slot * p.rows_pad + r_unit, make_float2(m_used, l_run));
+          if (c0 == 0) __stcg(p.ws_ml + (size_t)g.slot * p.rows_pad + r_unit, make_float2(m_used, l_run));
         }
         tc_fence_before_sync();   // O has been read: the next segment's first product overwrites it once this thread's P is announced
+        if (kSplit) {             // ... and the other chain's O and `fold`, once both have read them
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar_fold + 8);
+          ok = wait(bar_fold + 8, seg & 1);
+        }
+        ++seg;
       }
     }
   }
@@ -486,7 +534,7 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   tc_fence_before_sync();
   __syncthreads();
   if (tid == 0 && (*abort_ptr || *never_ptr)) dlm_set_status(p.status, DLM_ERR_TIMEOUT);
-  if (warp == 13) {
+  if (warp == kControl + 1) {
     tc_fence_after_sync();
     tmem_dealloc(tmem, kTmemCols);
     __syncwarp();
@@ -495,20 +543,21 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 
 // Joins the parts of split units.  Every boundary between two shares that lies inside a unit belongs to that unit; the first of them does
 // the work for all its parts.  Block = (boundary, 32 rows); a warp has 8 columns, a lane a row.
-template <int D>
-__global__ void __launch_bounds__(D * 4) q4_attention_join_kernel(const __grid_constant__ Params p, int grid) {
+template <int D, bool kFew>
+__global__ void __launch_bounds__(D * 4, 2) q4_attention_join_kernel(const __grid_constant__ Params p, int grid) {
   extern __shared__ int join_smem[];
   const Lengths len(join_smem, p.batch);
   dlm_grid_dependency_wait();
   dlm_trigger_dependents();
-  if (threadIdx.x < 32) read_lengths(p, len, nullptr);
+  constexpr int kKeys = kFew ? few::kKeys : kStep;
+  if (threadIdx.x < 32) read_lengths<kKeys>(p, len, nullptr);
   __syncthreads();
   const Deal d = deal_of(p, len, grid);
   const int c = blockIdx.x + 1;
   if (c >= d.n) return;
   const int boundary = d.lo(c);
   Segment g;
-  find_unit(p, len, d, boundary, g);
+  find_unit<kKeys>(p, len, d, boundary, g);
   if (g.unit_begin == boundary || d.lo(c - 1) > g.unit_begin) return;   // between two units; not the unit's first
   const int unit_end = g.unit_begin + len.prefix[g.b + 1] - len.prefix[g.b];
   const int c_first = c - 1, c_last = d.owner(unit_end - 1);
@@ -519,7 +568,7 @@ __global__ void __launch_bounds__(D * 4) q4_attention_join_kernel(const __grid_c
   const size_t out = (((size_t)g.layer * p.batch + g.b) * p.n_q_heads + (size_t)g.kvh * p.group) * p.q_cap + r_kv;
   // the part of block b: its first segment if the part starts where its share does, as all but the first part do, else its second
   const int first_slot = 2 * c_first + (d.lo(c_first) >= g.unit_begin ? 0 : 1);
-  constexpr int kAtOnce = 6;
+  constexpr int kAtOnce = 4;
   float m = -CUDART_INF_F, l = 0.f, o[8] = {};
 #pragma unroll 1
   for (int b0 = c_first; b0 <= c_last; b0 += kAtOnce) {
@@ -531,10 +580,10 @@ __global__ void __launch_bounds__(D * 4) q4_attention_join_kernel(const __grid_c
       x[j] = y[j] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (b0 + j <= c_last) {
         const size_t s = (size_t)(b0 + j == c_first ? first_slot : 2 * (b0 + j));
-        const float4* po = p.ws_o + (s * (D / 4) + 2 * c8) * p.rows_pad + row;
+        const float4* po = kFew ? p.ws_o + (s * p.rows_pad + row) * (D / 4) + 2 * c8 : p.ws_o + (s * (D / 4) + 2 * c8) * p.rows_pad + row;
         ml[j] = __ldcg(p.ws_ml + s * p.rows_pad + row);
         x[j] = __ldcg(po);
-        y[j] = __ldcg(po + p.rows_pad);
+        y[j] = __ldcg(po + (kFew ? 1 : p.rows_pad));
       }
     }
     float m_new = m;
@@ -561,19 +610,26 @@ __global__ void __launch_bounds__(D * 4) q4_attention_join_kernel(const __grid_c
   if (c8 == 0 && p.lse) p.lse[out] = active ? (m + lg2_approx(l)) * 0.6931471805599453f : -CUDART_INF_F;
 }
 
+// The kernels: few query rows a KV head (up to 16, up to 32), one M tile (up to 128), two; D 128 and 64; the last, with waits that do not wait.
 using Kernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const Params);
-Kernel kernel_of(int D, int n_mt, bool no_wait) {
-  if (D == 128) {
-    if (n_mt == 2) return no_wait ? q4_attention_kernel<128, 2, true> : q4_attention_kernel<128, 2, false>;
-    return no_wait ? q4_attention_kernel<128, 1, true> : q4_attention_kernel<128, 1, false>;
+constexpr int kKinds = 4;
+template <int D, bool kNoWait>
+Kernel kernel_of(int kind) {
+  switch (kind) {
+    case 0: return few::q4_attention_few_kernel<D, 16, kNoWait>;
+    case 1: return few::q4_attention_few_kernel<D, 32, kNoWait>;
+    case 2: return q4_attention_kernel<D, 1, kNoWait>;
+    default: return q4_attention_kernel<D, 2, kNoWait>;
   }
-  if (n_mt == 2) return no_wait ? q4_attention_kernel<64, 2, true> : q4_attention_kernel<64, 2, false>;
-  return no_wait ? q4_attention_kernel<64, 1, true> : q4_attention_kernel<64, 1, false>;
 }
-
-int shared_bytes(int D, int n_mt, int batch) {
-  const int tiles = D == 128 ? (n_mt == 2 ? Shape<128, 2>::kTiles : Shape<128, 1>::kTiles) : (n_mt == 2 ? Shape<64, 2>::kTiles : Shape<64, 1>::kTiles);
-  return 1024 + tiles + kBarrierBytes + kFlagBytes + 4 * length_ints(batch);
+template <int D>
+int tile_bytes(int kind) {
+  switch (kind) {
+    case 0: return few::Shape<D, 16>::kTiles + few::Shape<D, 16>::kExchange;
+    case 1: return few::Shape<D, 32>::kTiles + few::Shape<D, 32>::kExchange;
+    case 2: return Shape<D, 1>::kTiles + Shape<D, 1>::kFoldBytes;
+    default: return Shape<D, 2>::kTiles;
+  }
 }
 
 struct Workspace {
@@ -609,25 +665,30 @@ extern "C" int dlm_freecache_attn_step_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* c
   const int D = cache->head_dim, group = n_q_heads / cache->n_kv_heads, nl = layer_end - layer_begin;
   if (q_cap > kMaxQCap || (long long)group * q_cap > (1 << 20) || cache->batch > kMaxBatch) return DLM_ERR_UNSUPPORTED;
   if (((uintptr_t)q | (uintptr_t)k_new | (uintptr_t)v_new | (uintptr_t)out) & 15) return DLM_ERR_UNSUPPORTED;
-  const int rows_total = group * q_cap, n_mt = rows_total > 128 ? 2 : 1, chunk = 128 * n_mt, n_rc = (rows_total + chunk - 1) / chunk;
+  const int rows_total = group * q_cap, kind = rows_total <= 16 ? 0 : rows_total <= 32 ? 1 : rows_total <= 128 ? 2 : 3;
+  const bool is_few = kind < 2;
+  const int chunk = kind == 3 ? 256 : 128, n_rc = (rows_total + chunk - 1) / chunk;
   const long long units = (long long)nl * cache->batch * cache->n_kv_heads * n_rc;
-  const long long steps = (cache->capacity + kStep - 1) / kStep + (q_cap + kStep - 1) / kStep;
+  const int step = is_few ? few::kKeys : kStep;
+  const long long steps = (cache->capacity + step - 1) / step + (q_cap + step - 1) / step;
   if (units * steps >= (1LL << 30)) return DLM_ERR_UNSUPPORTED;   // items are counted in 32 bits
   DLM_DEVICE_TRY(ctx);
   const Workspace ws = workspace_of(ctx, D, rows_total);
   if (!workspace || workspace_bytes < ws.o_bytes + ws.ml_bytes || ((uintptr_t)workspace & 255)) return DLM_ERR_WORKSPACE;
   const bool no_wait = ctx->wait_limit_ns == 0;
-  const Kernel kern = kernel_of(D, n_mt, no_wait);
-  const int which = (D == 128 ? 0 : 1) + (n_mt == 2 ? 0 : 2) + (no_wait ? 4 : 0);
+  const Kernel kern = D == 128 ? (no_wait ? kernel_of<128, true>(kind) : kernel_of<128, false>(kind))
+                               : (no_wait ? kernel_of<64, true>(kind) : kernel_of<64, false>(kind));
+  const int which = kind + (D == 128 ? 0 : kKinds) + (no_wait ? 2 * kKinds : 0);
   if (ctx->q4_smem_limit[which] == 0) {
     cudaFuncAttributes a;
     DLM_CUDA_TRY(cudaFuncGetAttributes(&a, reinterpret_cast<const void*>(kern)));
-    if (a.numRegs != kRegsLaunch) return DLM_ERR_UNSUPPORTED;   // the register split would wait for ever
+    const int regs = is_few ? few::kRegsLaunch : kind == 2 ? Shape<64, 1>::kRegsLaunch : Shape<64, 2>::kRegsLaunch;
+    if (a.numRegs != regs) return DLM_ERR_UNSUPPORTED;   // the register split would wait for ever
     const int limit = ctx->max_smem_optin - (int)a.sharedSizeBytes;
     DLM_CUDA_TRY(cudaFuncSetAttribute(reinterpret_cast<const void*>(kern), cudaFuncAttributeMaxDynamicSharedMemorySize, limit));
     ctx->q4_smem_limit[which] = limit;
   }
-  const int smem = shared_bytes(D, n_mt, cache->batch);
+  const int smem = 1024 + (D == 128 ? tile_bytes<128>(kind) : tile_bytes<64>(kind)) + kBarrierBytes + kFlagBytes + 4 * length_ints(cache->batch);
   if (smem > ctx->q4_smem_limit[which]) return DLM_ERR_UNSUPPORTED;
   Params p;
   p.n_rc = n_rc;
@@ -653,7 +714,7 @@ extern "C" int dlm_freecache_attn_step_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* c
   p.chunk = chunk;
   p.rows = rows_total < chunk ? rows_total : chunk;
   p.rows_pad = (p.rows + 31) & ~31;
-  p.fresh_box = q_cap < kStep ? q_cap : kStep;
+  p.fresh_box = q_cap < step ? q_cap : step;
   p.min_share = 2;
   p.by_batch = make_fast_div(p.batch);
   p.by_rc = make_fast_div(p.n_rc);
@@ -667,16 +728,15 @@ extern "C" int dlm_freecache_attn_step_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* c
   if (rc == DLM_OK) rc = encode_rows_map(ctx, &tm_kn, k_new, D, q_cap, slabs, p.fresh_box);
   if (rc == DLM_OK) rc = encode_rows_map(ctx, &tm_vn, v_new, D, q_cap, slabs, p.fresh_box);
   if (rc != DLM_OK) return rc;
-  const long long most = units * steps;
+  const long long most = (units * steps + p.min_share - 1) / p.min_share;   // blocks with work, at full capacity
   const int sms = ctx->num_sms < kMaxGrid ? ctx->num_sms : kMaxGrid, grid = most < sms ? (int)most : sms;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  DLM_CUDA_TRY(dlm_launch(kern, dim3(grid), dim3(kThreads), (size_t)smem, st, tm_q, tm_kn, tm_vn, p));
+  DLM_CUDA_TRY(dlm_launch(kern, dim3(grid), dim3(is_few ? few::kThreads : kind == 2 ? Shape<64, 1>::kThreads : Shape<64, 2>::kThreads), (size_t)smem, st, tm_q, tm_kn, tm_vn, p));
   if (grid == 1) return dlm_launch_ok(ctx, 1);
   const dim3 join((unsigned)(grid - 1), (unsigned)(p.rows_pad / 32));
   const size_t join_smem = 4 * (size_t)length_ints(cache->batch);
-  if (D == 128)
-    DLM_CUDA_TRY(dlm_launch(q4_attention_join_kernel<128>, join, dim3(512), join_smem, st, p, grid));
-  else
-    DLM_CUDA_TRY(dlm_launch(q4_attention_join_kernel<64>, join, dim3(256), join_smem, st, p, grid));
+  void (*const join_kern)(const Params, int) = D == 128 ? (is_few ? q4_attention_join_kernel<128, true> : q4_attention_join_kernel<128, false>)
+                                                        : (is_few ? q4_attention_join_kernel<64, true> : q4_attention_join_kernel<64, false>);
+  DLM_CUDA_TRY(dlm_launch(join_kern, join, dim3(D * 4), join_smem, st, p, grid));
   return dlm_launch_ok(ctx, 2);
 }

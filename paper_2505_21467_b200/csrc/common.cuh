@@ -64,7 +64,7 @@ struct dlm_ctx {
   dlm_attn_plan attn_plan;
   int attn_clusters[17];        // clusters of so many attention blocks that the device runs at a time (0 = not asked yet, -1 = none)
   int attn_smem_limit[32];      // dynamic shared memory the attention kernels may use on this device (0 = not set up yet)
-  int q4_smem_limit[8];         // ... those of the 4-bit cache
+  int q4_smem_limit[16];         // ... those of the 4-bit cache
   int weight_smem_limit[4];     // ... the kernels that accumulate weights
 };
 
