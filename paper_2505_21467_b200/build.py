@@ -48,6 +48,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if proc.returncode != 0:
         raise RuntimeError("nvcc failed building libdlm.so")
     check_attention_registers(proc.stdout)
+    check_q4_attention_registers(proc.stdout)
     os.replace(tmp, LIB)
     build_calls(force=force, verbose=verbose)
     return LIB
@@ -117,21 +118,42 @@ def build_calls(force: bool = False, verbose: bool = False) -> str:
 ATTENTION_REGISTERS = 168
 
 
-def check_attention_registers(ptxas_log: str) -> None:
-    seen, name = 0, None
+def kernel_registers(ptxas_log: str) -> list:
+    """[(kernel, registers a thread)] of a ptxas log."""
+    found, name = [], None
     for line in ptxas_log.splitlines():
         if "Compiling entry function" in line:
             name = line.split("'")[1] if "'" in line else line
         elif "Used" in line and "registers" in line and name is not None:
-            if "attn_step_sm100_kernel" in name:
-                seen += 1
-                regs = int(line.split("Used")[1].split("registers")[0])
-                if regs != ATTENTION_REGISTERS:
-                    raise RuntimeError(f"{name}: ptxas allocated {regs} registers, the kernel's register split needs "
-                                       f"{ATTENTION_REGISTERS}")
+            found.append((name, int(line.split("Used")[1].split("registers")[0])))
             name = None
-    if seen == 0:
+    return found
+
+
+def check_attention_registers(ptxas_log: str) -> None:
+    kernels = [(name, regs) for name, regs in kernel_registers(ptxas_log) if "attn_step_sm100_kernel" in name]
+    for name, regs in kernels:
+        if regs != ATTENTION_REGISTERS:
+            raise RuntimeError(f"{name}: ptxas allocated {regs} registers, the kernel's register split needs "
+                               f"{ATTENTION_REGISTERS}")
+    if not kernels:
         raise RuntimeError("no attention kernel found in the ptxas log: cannot check its register count")
+
+
+# The same for the attention over a 4-bit cache (attn_step_q4.cu, attn_q4_few.cuh: kRegsLaunch), by what its mangled name has.
+Q4_ATTENTION_REGISTERS = {"q4_attention_kernelILi64ELi1E": 96, "q4_attention_kernelILi128ELi1E": 96, "q4_attention_kernelILi64ELi2E": 128,
+                          "q4_attention_kernelILi128ELi2E": 128, "q4_attention_few_kernel": 72}
+
+
+def check_q4_attention_registers(ptxas_log: str) -> None:
+    kernels = kernel_registers(ptxas_log)
+    for part, want in Q4_ATTENTION_REGISTERS.items():
+        of_kind = [(name, regs) for name, regs in kernels if part in name]
+        if not of_kind:
+            raise RuntimeError(f"no kernel {part}.. found in the ptxas log: cannot check its register count")
+        for name, regs in of_kind:
+            if regs != want:
+                raise RuntimeError(f"{name}: ptxas allocated {regs} registers, the kernel's register split needs {want}")
 
 
 if __name__ == "__main__":

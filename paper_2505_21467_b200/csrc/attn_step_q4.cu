@@ -656,7 +656,6 @@ extern "C" int dlm_freecache_attn_step_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* c
                                           const void* k_new, const void* v_new, int n_q_heads, int q_cap, const int32_t* q_len,
                                           float softmax_scale, int cache_len_hint, void* out, float* lse, void* workspace,
                                           size_t workspace_bytes, void* stream) {
-  (void)cache_len_hint;
   if (!ctx || !q || !k_new || !v_new || !out) return DLM_ERR_NULL;
   const int bad = dlm_check_q4(cache);
   if (bad != DLM_OK) return bad;
@@ -728,7 +727,9 @@ extern "C" int dlm_freecache_attn_step_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* c
   if (rc == DLM_OK) rc = encode_rows_map(ctx, &tm_kn, k_new, D, q_cap, slabs, p.fresh_box);
   if (rc == DLM_OK) rc = encode_rows_map(ctx, &tm_vn, v_new, D, q_cap, slabs, p.fresh_box);
   if (rc != DLM_OK) return rc;
-  const long long most = (units * steps + p.min_share - 1) / p.min_share;   // blocks with work, at full capacity
+  // blocks that find work if the cache is as long as expected (else fewer blocks have more)
+  const int expected = cache_len_hint > 0 && cache_len_hint < cache->capacity ? cache_len_hint : cache->capacity;
+  const long long most = (units * ((expected + step - 1) / step + (q_cap + step - 1) / step) + p.min_share - 1) / p.min_share;
   const int sms = ctx->num_sms < kMaxGrid ? ctx->num_sms : kMaxGrid, grid = most < sms ? (int)most : sms;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   DLM_CUDA_TRY(dlm_launch(kern, dim3(grid), dim3(is_few ? few::kThreads : kind == 2 ? Shape<64, 1>::kThreads : Shape<64, 2>::kThreads), (size_t)smem, st, tm_q, tm_kn, tm_vn, p));

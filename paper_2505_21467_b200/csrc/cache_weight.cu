@@ -462,8 +462,8 @@ using Kernel = void (*)(const CUtensorMap, const CUtensorMap, const Params);
 
 template <bool kQ4, typename Cache>
 int accumulate(dlm_ctx* ctx, const Cache* cache, const uint8_t* k_scale, int layer_begin, int layer_end, const void* q, const float* lse,
-               int n_q_heads, int q_cap, const int32_t* q_len, float softmax_scale, const float* collected, float decay, float* weight,
-               void* stream) {
+               int n_q_heads, int q_cap, const int32_t* q_len, float softmax_scale, int cache_len_hint, const float* collected, float decay,
+               float* weight, void* stream) {
   if (n_q_heads <= 0 || q_cap <= 0 || layer_begin < 0 || layer_end > cache->n_layers || layer_begin >= layer_end) return DLM_ERR_SHAPE;
   const int D = cache->head_dim;
   if ((D != 64 && D != 128) || n_q_heads % cache->n_kv_heads != 0 || decay != decay) return DLM_ERR_UNSUPPORTED;
@@ -520,7 +520,9 @@ int accumulate(dlm_ctx* ctx, const Cache* cache, const uint8_t* k_scale, int lay
   if (!kQ4 && rc == DLM_OK)
     rc = encode_rows_map(ctx, &tm_k, cache->k, D, cache->capacity, (long long)cache->n_layers * cache->batch * cache->n_kv_heads, p.k_box);
   if (rc != DLM_OK) return rc;
-  const int sms = ctx->num_sms < kMaxGrid ? ctx->num_sms : kMaxGrid, grid = units * tiles < sms ? (int)(units * tiles) : sms;
+  const int sms = ctx->num_sms < kMaxGrid ? ctx->num_sms : kMaxGrid, expected = cache_len_hint > 0 && cache_len_hint < cache->capacity ? cache_len_hint : cache->capacity;
+  const long long most = units * ((expected + kKeys - 1) / kKeys);   // blocks that find work if the cache is as long as expected
+  const int grid = most < sms ? (int)most : sms;
   DLM_CUDA_TRY(dlm_launch(kern, dim3(grid), dim3(threads), (size_t)smem, static_cast<cudaStream_t>(stream), tm_q, tm_k, p));
   return dlm_launch_ok(ctx, 1);
 }
@@ -530,20 +532,18 @@ int accumulate(dlm_ctx* ctx, const Cache* cache, const uint8_t* k_scale, int lay
 extern "C" int dlm_cache_weight_accumulate(dlm_ctx* ctx, const dlm_kv_cache* cache, int layer_begin, int layer_end, const void* q,
                                            const float* lse, int n_q_heads, int q_cap, const int32_t* q_len, float softmax_scale,
                                            int cache_len_hint, const float* collected, float decay, float* weight, void* stream) {
-  (void)cache_len_hint;
   if (!ctx || !cache || !cache->k || !cache->cache_len || !q || !lse || !weight) return DLM_ERR_NULL;
   if (cache->n_layers <= 0 || cache->batch <= 0 || cache->n_kv_heads <= 0 || cache->capacity <= 0) return DLM_ERR_SHAPE;
-  return accumulate<false>(ctx, cache, nullptr, layer_begin, layer_end, q, lse, n_q_heads, q_cap, q_len, softmax_scale, collected, decay,
-                           weight, stream);
+  return accumulate<false>(ctx, cache, nullptr, layer_begin, layer_end, q, lse, n_q_heads, q_cap, q_len, softmax_scale, cache_len_hint, collected,
+                           decay, weight, stream);
 }
 
 extern "C" int dlm_cache_weight_accumulate_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* cache, int layer_begin, int layer_end, const void* q,
                                               const float* lse, int n_q_heads, int q_cap, const int32_t* q_len, float softmax_scale,
                                               int cache_len_hint, const float* collected, float decay, float* weight, void* stream) {
-  (void)cache_len_hint;
   if (!ctx || !q || !lse || !weight) return DLM_ERR_NULL;
   const int bad = dlm_check_q4(cache);
   if (bad != DLM_OK) return bad;
   return accumulate<true>(ctx, cache, static_cast<const uint8_t*>(cache->k_scale), layer_begin, layer_end, q, lse, n_q_heads, q_cap, q_len,
-                          softmax_scale, collected, decay, weight, stream);
+                          softmax_scale, cache_len_hint, collected, decay, weight, stream);
 }

@@ -428,29 +428,6 @@ __device__ __forceinline__ float ex2_approx(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// max(a, b), NaN if either is.
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float y;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
-  return y;
-}
-// 2^x of a pair without the special function unit, for -127 <= x <= 126 (0 for -127; other x must not be given): x = n + f with n whole and |f| <= 1/2
-// by adding and taking away 1.5 * 2^23; 2^f by a polynomial of degree 5 (fitted for the least largest relative error, 1.6e-7 with its
-// rounding; p(0) = 1), whose exponent field n is then added to.
-__device__ __forceinline__ void exp2_pair(uint64_t x, float& y0, float& y1) {
-  const float kShift = 12582912.f;
-  const uint64_t t = add2(x, pack2(kShift, kShift)), f = fma2(add2(t, pack2(-kShift, -kShift)), pack2(-1.f, -1.f), x);
-  uint64_t p = fma2(f, pack2(0.001326472731307149f, 0.001326472731307149f), pack2(0.009671512991189957f, 0.009671512991189957f));
-  p = fma2(f, p, pack2(0.05550733581185341f, 0.05550733581185341f));
-  p = fma2(f, p, pack2(0.24022242426872253f, 0.24022242426872253f));
-  p = fma2(f, p, pack2(0.6931470036506653f, 0.6931470036506653f));
-  p = fma2(f, p, pack2(1.f, 1.f));
-  float p0, p1, t0, t1;
-  unpack2(p, p0, p1);
-  unpack2(t, t0, t1);
-  y0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23));
-  y1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23));
-}
 __device__ __forceinline__ float lg2_approx(float x) {
   float y;
   asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
