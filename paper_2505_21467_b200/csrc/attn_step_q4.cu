@@ -547,27 +547,34 @@ template <int D, bool kFew>
 __global__ void __launch_bounds__(D * 4, 2) q4_attention_join_kernel(const __grid_constant__ Params p, int grid) {
   extern __shared__ int join_smem[];
   const Lengths len(join_smem, p.batch);
-  dlm_grid_dependency_wait();
-  dlm_trigger_dependents();
   constexpr int kKeys = kFew ? few::kKeys : kStep;
+  // The lengths are not written by the attention kernel, and this one starts only when every block of that has waited for those before:
+  // what is to be joined is found while its parts are still computed.
   if (threadIdx.x < 32) read_lengths<kKeys>(p, len, nullptr);
   __syncthreads();
   const Deal d = deal_of(p, len, grid);
   const int c = blockIdx.x + 1;
-  if (c >= d.n) return;
-  const int boundary = d.lo(c);
-  Segment g;
-  find_unit<kKeys>(p, len, d, boundary, g);
-  if (g.unit_begin == boundary || d.lo(c - 1) > g.unit_begin) return;   // between two units; not the unit's first
-  const int unit_end = g.unit_begin + len.prefix[g.b + 1] - len.prefix[g.b];
-  const int c_first = c - 1, c_last = d.owner(unit_end - 1);
+  bool joins = c < d.n;
+  Segment g = {};
+  int c_first = 0, c_last = 0, first_slot = 0;
+  if (joins) {
+    const int boundary = d.lo(c);
+    find_unit<kKeys>(p, len, d, boundary, g);
+    joins = g.unit_begin != boundary && d.lo(c - 1) <= g.unit_begin;   // inside a unit, and its first
+    const int unit_end = g.unit_begin + len.prefix[g.b + 1] - len.prefix[g.b];
+    c_first = c - 1;
+    c_last = d.owner(unit_end - 1);
+    // the part of block b: its first segment if the part starts where its share does, as all but the first part do, else its second
+    first_slot = 2 * c_first + (d.lo(c_first) >= g.unit_begin ? 0 : 1);
+  }
+  dlm_grid_dependency_wait();
+  dlm_trigger_dependents();
+  if (!joins) return;
   const int row = blockIdx.y * 32 + (threadIdx.x & 31), c8 = threadIdx.x >> 5;
   const int r_kv = g.rc * p.chunk + row;
   if (row >= p.rows || r_kv >= p.rows_total) return;
   const bool active = r_kv - p.by_q_cap.div(r_kv) * p.q_cap < g.Lq;
   const size_t out = (((size_t)g.layer * p.batch + g.b) * p.n_q_heads + (size_t)g.kvh * p.group) * p.q_cap + r_kv;
-  // the part of block b: its first segment if the part starts where its share does, as all but the first part do, else its second
-  const int first_slot = 2 * c_first + (d.lo(c_first) >= g.unit_begin ? 0 : 1);
   constexpr int kAtOnce = 4;
   float m = -CUDART_INF_F, l = 0.f, o[8] = {};
 #pragma unroll 1
