@@ -141,7 +141,7 @@ def check_attention_registers(ptxas_log: str) -> None:
 
 
 # The same for the attention over a 4-bit cache (attn_step_q4.cu, attn_q4_few.cuh: kRegsLaunch), by what its mangled name has.
-Q4_ATTENTION_REGISTERS = {"q4_attention_kernelILi64ELi1E": 72, "q4_attention_kernelILi128ELi1E": 72, "q4_attention_kernelILi64ELi2E": 128,
+Q4_ATTENTION_REGISTERS = {"q4_attention_kernelILi64ELi1E": 96, "q4_attention_kernelILi128ELi1E": 96, "q4_attention_kernelILi64ELi2E": 128,
                           "q4_attention_kernelILi128ELi2E": 128, "q4_attention_few_kernel": 72}
 
 

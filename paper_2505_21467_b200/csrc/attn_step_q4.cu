@@ -38,9 +38,9 @@ constexpr int kBarrierBytes = 512, kFlagBytes = 64;
 template <int D, int NMT>
 struct Shape {
   static constexpr bool kSplit = NMT == 1;                   // the chains share an M tile and split the steps
-  static constexpr int kDecodeWarps = kSplit ? 16 : 4, kTeamWarps = kDecodeWarps / 4, kControl = 8 + kDecodeWarps, kThreads = 32 * (kControl + 4);
+  static constexpr int kDecodeWarps = kSplit ? 8 : 4, kTeamWarps = kDecodeWarps / 4, kControl = 8 + kDecodeWarps, kThreads = 32 * (kControl + 4);
   // registers a thread: at launch all of the SM's, then by role
-  static constexpr int kRegsLaunch = kSplit ? 72 : 128, kRegsSoftmax = kSplit ? 112 : 168, kRegsDecode = kSplit ? 56 : 104, kRegsControl = kSplit ? 56 : 72;
+  static constexpr int kRegsLaunch = kSplit ? 96 : 128, kRegsSoftmax = kSplit ? 136 : 168, kRegsDecode = kSplit ? 72 : 104, kRegsControl = kSplit ? 64 : 72;
   static_assert(8 * kRegsSoftmax + kDecodeWarps * kRegsDecode + 4 * kRegsControl <= (kControl + 4) * kRegsLaunch, "register split");
   static constexpr int kPanels = D / 64;
   static constexpr int kQPanel = 128 * 128;                  // bytes: 128 rows of 64 values
