@@ -6,8 +6,9 @@
 // 128 threads has a key and works along the query rows; O^T = V^T P^T has a value column a lane.  What a softmax needs across keys is
 // then across threads, and is avoided: P = 2^(s - m) for a reference m per query row that need not be its maximum.  P is bf16 and
 // sums are fp32, whose range is that of 2^127, so the reference is the score of the first key of a group's first tile, kept for the rest
-// of the segment unless some score exceeds it by 2^60 (then every thread of the group learns of it before P is used, and m, the sums and O^T are moved
-// to the tile's maximum).  Sums are per thread and added up once, at the end of the segment, in a fixed order.
+// of the segment unless some score exceeds it by 30 (then every thread of the group learns of it before P is used, m becomes the tile's largest
+// score, and the sums and O^T are moved to it).  A first score that is not finite is no reference: the lowest number stands in for it, which any
+// finite score then replaces.  Sums are per thread and added up once, at the end of the segment, in a fixed order.
 //
 // Steps ("tiles") of 128 keys, dealt in turn to two groups of four warps, each with an O^T, references and sums of its own.  Block = 28 warps:
 //   warps 0-3, 4-7    the groups
@@ -22,7 +23,15 @@ constexpr int kThreads = 896;
 constexpr int kKeys = 128;
 constexpr int kRegsLaunch = 72, kRegsGroup = 96, kRegsDecode = 64, kRegsControl = 56;
 static_assert(2 * kRegsGroup + 4 * kRegsDecode + kRegsControl <= 7 * kRegsLaunch, "register split");
-constexpr uint32_t kTooLarge = (127u + 60u) << 7;   // bf16 of 2^60
+constexpr uint32_t kTooLarge = (127u + 30u) << 7;   // bf16 of 2^30: P of a segment's keys times values up to 2^80 sums up in fp32
+constexpr float kLowest = -3.402823466e38f;
+
+// Numbers as unsigned integers in the same order; 0 is none of them.
+__device__ __forceinline__ uint32_t to_ordered(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return u >> 31 ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float from_ordered(uint32_t o) { return __uint_as_float(o >> 31 ? o & 0x7FFFFFFFu : ~o); }
 
 template <int D, int N>
 struct Shape {
@@ -36,7 +45,7 @@ struct Shape {
   static constexpr int KS = 2, VS = 2, kDepthP = D == 128 ? 3 : 6, PS = 2 * kDepthP;
   // (P behind V: with heads of 64 the products read a second panel behind a V tile, whose rows of O^T nobody reads)
   static constexpr int kTiles = (KS + VS) * kTile + 2 * kPTile + kQTile + PS * kPackedStage;
-  // floats: minus the references [2][N], parts of sums [2][4][N], weights of the groups [2][N], largest excess [2][N]
+  // floats: minus the references [2][N], parts of sums [2][4][N], weights of the groups [2][N], next references [2][N]
   static constexpr int kExchange = 4 * (2 + 8 + 2 + 2) * N;
   static constexpr uint32_t kColS = 0, kColO = 256;             // S^T: [group][buffer] of 64 columns; O^T: [group] of 64
 };
@@ -80,7 +89,7 @@ q4_attention_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
   float* const minus_m = xch;              // [group][N], log2 units
   float* const sums = xch + 2 * N;         // [group][warp][N]
   float* const share = xch + 10 * N;       // [group][N]: what O^T of the group is multiplied with
-  int* const excess = reinterpret_cast<int*>(xch + 12 * N);   // [group][N]: bits of the largest exponent above the reference (0: none)
+  uint32_t* const next_m = reinterpret_cast<uint32_t*>(xch + 12 * N);   // [group][N]: the largest score above the reference (to_ordered; 0: none)
   int* const flags = reinterpret_cast<int*>(smem_raw + smem_pad + G::kTiles + G::kExchange + kBarrierBytes);
   volatile int* const abort_ptr = flags;
   volatile int* const never_ptr = flags + 1;
@@ -131,7 +140,7 @@ q4_attention_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
     mbar_fence_init();
     fence_proxy_async_smem();
   }
-  if (tid < 2 * N) excess[tid] = 0;
+  if (tid < 2 * N) next_m[tid] = 0;
   if (warp == 25) {
     tmem_alloc(smem_u32(tmem_slot), kTmemCols);
     tmem_relinquish();
@@ -362,8 +371,8 @@ q4_attention_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
               if (lane == 0) {
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                  const float m = __uint_as_float(v[j]) * p.scale_log2;
-                  minus_m[w * N + c + j] = fabsf(m) < 1e30f ? -m : 0.f;
+                  const float m = __fmul_ru(__uint_as_float(v[j]), p.scale_log2);   // (up: scaled_maximum)
+                  minus_m[w * N + c + j] = fabsf(m) <= -kLowest ? -m : -kLowest;
                 }
               }
             }
@@ -417,13 +426,15 @@ q4_attention_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
         if (!ok) break;
         if (too_large[w] == n_own + 1) {
           // ---- rare: the tile's maxima become the references, for the query rows where they are larger
-          auto exponents = [&](int c, float (&x)[8]) {
+          auto scores = [&](int c, float (&x)[8]) {
             uint32_t one[8];
             tmem_ld8(t_s + c, one);
             tmem_ld_wait();
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = fmaf(__uint_as_float(one[j]), p.scale_log2, minus_m[w * N + c + j]);
+            for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(one[j]);
           };
+          // (differences of two references are as good as the references; a score is only ever taken against one of them, in one rounding)
+          auto minus_next = [&](int i) { return next_m[i] ? -from_ordered(next_m[i]) : minus_m[i]; };
           auto meet = [&]() {
             __syncwarp();
             if (lane == 0) mbar_arrive(bar_slow + 8 * w);
@@ -432,27 +443,31 @@ q4_attention_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
           float x[8];
 #pragma unroll 1
           for (int c = 0; c < N; c += 8) {
-            exponents(c, x);
+            scores(c, x);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-              const int top = __reduce_max_sync(0xffffffffu, valid && x[j] > 0.f ? __float_as_int(x[j]) : 0);
-              if (lane == 0 && top > 0) atomicMax(&excess[w * N + c + j], top);
+              const bool above = valid && fmaf(x[j], p.scale_log2, minus_m[w * N + c + j]) > 0.f;
+              const uint32_t top = __reduce_max_sync(0xffffffffu, above ? to_ordered(__fmul_ru(x[j], p.scale_log2)) : 0u);
+              if (lane == 0 && top > 0) atomicMax(&next_m[w * N + c + j], top);
             }
           }
           ok = meet();
           if (!ok) break;
 #pragma unroll
           for (int c = 0; c < N; c += 8) {
-            exponents(c, x);
+            scores(c, x);
 #pragma unroll
             for (int j = 0; j < 8; j += 2) {
-              const float e0 = __int_as_float(excess[w * N + c + j]), e1 = __int_as_float(excess[w * N + c + j + 1]);
-              float a, d;
-              unpack2(l2[(c + j) / 2], a, d);
-              // (a sum with a term above 2^100 is that term, as far as fp32 holds it)
-              a = valid && x[j] > 100.f ? ex2_approx(x[j] - e0) : a * ex2_approx(-e0);
-              d = valid && x[j + 1] > 100.f ? ex2_approx(x[j + 1] - e1) : d * ex2_approx(-e1);
-              l2[(c + j) / 2] = pack2(a, d);
+              float l[2];
+              unpack2(l2[(c + j) / 2], l[0], l[1]);
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const int i = w * N + c + j + k;
+                const float next = minus_next(i);
+                // (a sum with a term above 2^100 is that term, as far as fp32 holds it)
+                l[k] = valid && fmaf(x[j + k], p.scale_log2, minus_m[i]) > 100.f ? ex2_approx(fmaf(x[j + k], p.scale_log2, next)) : l[k] * ex2_approx(next - minus_m[i]);
+              }
+              l2[(c + j) / 2] = pack2(l[0], l[1]);
             }
           }
           if (n_own > n_first) {                                   // the group's products so far are complete (pv_done above)
@@ -462,7 +477,7 @@ q4_attention_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
               tmem_ld16(t_o + c, v);
               tmem_ld_wait();
 #pragma unroll
-              for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * ex2_approx(-__int_as_float(excess[w * N + c + j])));
+              for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * ex2_approx(minus_next(w * N + c + j) - minus_m[w * N + c + j]));
               tmem_st16(t_o + c, v);
             }
             tmem_st_wait();
@@ -470,8 +485,8 @@ q4_attention_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
           ok = meet();
           if (!ok) break;
           if (key < N) {
-            minus_m[w * N + key] -= __int_as_float(excess[w * N + key]);
-            excess[w * N + key] = 0;
+            minus_m[w * N + key] = minus_next(w * N + key);
+            next_m[w * N + key] = 0;
           }
           ok = meet();
           if (!ok) break;

@@ -23,6 +23,13 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 // the same maximum, cancels it.  Ragged half-steps compare maxima (kRescaleThreshold, log2 units);
 // full ones look at the row sum (kSumLimit).
 // (real = false: nobody reads the thread's row, which may hold anything; it does not take the warp through a rescaling.)
+// kFloor: for scores of any size.  A half-step of nothing but -infinity leaves the lowest number as the maximum and 0 as the sum (else both are NaN
+// from there on), and the maximum is rounded up, so that scores below -2^30, which are further than 1 apart, give no 2^(s - m) above 1.
+constexpr float kLowestMaximum = -3.402823466e38f;
+template <bool kFloor>
+__device__ __forceinline__ float scaled_maximum(float mx, float scale_log2) {
+  return kFloor ? fmaxf(__fmul_ru(mx, scale_log2), kLowestMaximum) : mx * scale_log2;
+}
 constexpr float kRescaleThreshold = 8.0f;
 
 // Rare path shared by both kinds of half-step: some row of the warp outgrew its maximum by more
@@ -97,7 +104,7 @@ __device__ __forceinline__ float exp64_store(const uint32_t (&s)[64], float scal
   return l0 + l1;
 }
 
-template <int D>
+template <int D, bool kFloor = false>
 __device__ __forceinline__ bool softmax_half_full(uint32_t t_s, uint32_t t_o, bool first, float scale_log2,
                                                   float& m_used, float& l_run, uint32_t bar_pv_done,
                                                   uint32_t pv_parity, volatile int* abort_ptr, bool real = true) {
@@ -106,14 +113,14 @@ __device__ __forceinline__ bool softmax_half_full(uint32_t t_s, uint32_t t_o, bo
   tmem_ld32(t_s + 32, s + 32);
   tmem_ld_wait();
   if (first) {
-    m_used = row_max64<D>(s) * scale_log2;
+    m_used = scaled_maximum<kFloor>(row_max64<D>(s), scale_log2);
     l_run = 0.f;
   }
   float l_half = exp64_store(s, scale_log2, m_used, t_s);
   if (!first) {
     const bool grow = real && !(l_half <= kSumLimit);   // also catches a NaN sum
     if (__any_sync(0xffffffffu, grow)) {
-      const float m_new = row_max64<D>(s) * scale_log2;
+      const float m_new = scaled_maximum<kFloor>(row_max64<D>(s), scale_log2);
       tmem_st_wait();   // the P just written is replaced below
       if (!rescale_o<D>(t_o, grow, m_new, m_used, l_run, bar_pv_done, pv_parity, abort_ptr)) return false;
       l_half = exp64_store(s, scale_log2, m_used, t_s);
@@ -126,7 +133,7 @@ __device__ __forceinline__ bool softmax_half_full(uint32_t t_s, uint32_t t_o, bo
 
 // Ragged half-step (fewer than 64 valid keys: the end of the cache rows, or the fresh rows): 32
 // columns at a time, keys at or beyond `valid` masked out.
-template <int D>
+template <int D, bool kFloor = false>
 __device__ __noinline__ bool softmax_half_ragged(uint32_t t_s, uint32_t t_o, int valid, bool first, float scale_log2,
                                                  float& m_used, float& l_run, uint32_t bar_pv_done,
                                                  uint32_t pv_parity, volatile int* abort_ptr, bool real = true) {
@@ -140,7 +147,7 @@ __device__ __noinline__ bool softmax_half_ragged(uint32_t t_s, uint32_t t_o, int
     for (int j = 0; j < 32; ++j)
       if (c * 32 + j < valid) mx = fmaxf(mx, __uint_as_float(v[j]));
   }
-  const float m_new = mx * scale_log2;
+  const float m_new = scaled_maximum<kFloor>(mx, scale_log2);
   if (first) {
     m_used = m_new;
     l_run = 0.f;

@@ -441,9 +441,9 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           tc_fence_after_sync();
           const int keys = step_keys(g, t);
           if (keys == kStep)
-            ok = softmax_half_full<D>(t_s + buf * kStep, t_o, t == first, p.scale_log2, m_used, l_run, bar_pv_done + before, parity, abort_ptr, active);
+            ok = softmax_half_full<D, true>(t_s + buf * kStep, t_o, t == first, p.scale_log2, m_used, l_run, bar_pv_done + before, parity, abort_ptr, active);
           else
-            ok = softmax_half_ragged<D>(t_s + buf * kStep, t_o, keys, t == first, p.scale_log2, m_used, l_run, bar_pv_done + before, parity, abort_ptr, active);
+            ok = softmax_half_ragged<D, true>(t_s + buf * kStep, t_o, keys, t == first, p.scale_log2, m_used, l_run, bar_pv_done + before, parity, abort_ptr, active);
           if (!ok) break;
           __syncwarp();
           if (lane == 0) {

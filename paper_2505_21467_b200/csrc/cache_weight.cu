@@ -488,7 +488,7 @@ int accumulate(dlm_ctx* ctx, const Cache* cache, const uint8_t* k_scale, int lay
   p.lse = lse;
   p.collected = collected;
   p.weight = weight;
-  p.decay = decay;
+  p.decay = collected ? decay : 0.f;
   p.nl = nl;
   p.layer_begin = layer_begin;
   p.batch = cache->batch;

@@ -256,3 +256,62 @@ def test_hints_of_any_size_give_the_same_results(dev):
         check_attention(c, q, kn, vn, [10, 10], out, lse)
         w, _ = ref.weights(c.values("k", 1), [1000, 20], q[1], lse[1].cpu(), [10, 10], None, 1.0)
         assert torch.allclose(weight[1, 0, :, :1000].cpu().double(), w[0, :, :1000], rtol=1e-4)
+
+
+@pytest.mark.parametrize("low", [-math.inf, -3e38, -1e30, -3e4])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("g,L", [(1, 3), (2, 15), (4, 20), (6, 40)])
+def test_fresh_keys_far_below_the_others(dev, g, L, D, low):
+    """Fresh rows whose scores are the lowest numbers or -infinity for every query have no weight, wherever they are: as the first key, as the only ones
+    of a tile or of a block's part.  The others' weights are as if those rows were not there (differences of thousands of units are 0 in 64 bits too)."""
+    for cached in (0, 5, 64, 130, 3000):
+        c = Cache(dev, 1, 1, 1, (cached + 8) // 8 * 8, D, [cached], 291)
+        q, kn, vn = inputs(1, 1, g, 1, L, D, [L], 292)
+        q[..., 0] = q[..., 0].abs() + 1
+        for rows in (slice(0, 1), slice(0, L - 1), slice(0, L)):
+            if rows.stop == L and cached == 0:
+                continue
+            low_kn = kn.clone()
+            low_kn[..., rows, 0] = low
+            out, lse = (t.cpu() for t in attention_call(dev, c, q.cuda(), low_kn.cuda(), vn.cuda(), None))
+            assert dev.status() == 0
+            want, w_lse, spread, size = ref.attention(c.values("k", 0), c.values("v", 0), [cached], q[0], kn[0, :, :, rows.stop:], vn[0, :, :, rows.stop:], [L])
+            off = size * 2 * D * 2.0 ** -24 + 2.0 ** -20              # as check_attention has it
+            tol = 2.0 ** -8 * (spread + want.abs()) * (1 + 2.0 ** -6) + 2 * off[..., None] * spread + 2.0 ** -110
+            assert bool(((out[0].double() - want).abs() <= tol).all()), (cached, rows)
+            assert bool(((lse[0].double() - w_lse).abs() <= off + 2.0 ** -22 * (w_lse.abs() + 8)).all()), (cached, rows)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("g,L", [(1, 3), (2, 15), (4, 20), (6, 40)])
+def test_a_first_key_far_below_and_scores_that_differ_among_the_others(dev, g, L, D):
+    """The first key's score is no scale for the others': theirs differ by tens of units and keep their differences."""
+    cached = 700
+    c = Cache(dev, 1, 1, 1, 704, D, [cached], 301)
+    k = torch.randn(1, 1, 1, 704, D, generator=torch.Generator().manual_seed(302)) * 4
+    k[..., 0, :] = 0
+    k[..., 0, :32] = -26000.0
+    k[..., 128, :32] = -20000.0
+    c.host["k"], c.host["k_scale"] = ref.pack(*ref.quantise(k.bfloat16()))
+    c.gpu["k"].copy_(c.host["k"]), c.gpu["k_scale"].copy_(c.host["k_scale"])
+    q, kn, vn = inputs(1, 1, g, 1, L, D, [L], 303)
+    q[..., :32] = q[..., :32].abs() + 0.5
+    out, lse = (t.cpu() for t in attention_call(dev, c, q.cuda(), kn.cuda(), vn.cuda(), None))
+    assert dev.status() == 0
+    seen = torch.ones(cached, dtype=torch.bool)
+    seen[0] = seen[128] = False                                     # scores below -10^4: no weight
+    want, w_lse, spread, size = ref.attention(c.values("k", 0)[:, :, :cached][:, :, seen], c.values("v", 0)[:, :, :cached][:, :, seen], [cached - 2], q[0], kn[0], vn[0], [L])
+    off = size * 2 * D * 2.0 ** -24 + 2.0 ** -20
+    tol = 2.0 ** -8 * (spread + want.abs()) * (1 + 2.0 ** -6) + 2 * off[..., None] * spread + 2.0 ** -110
+    assert bool(((out[0].double() - want).abs() <= tol).all())
+    assert bool(((lse[0].double() - w_lse).abs() <= off + 2.0 ** -22 * (w_lse.abs() + 8)).all())
+
+
+def test_nothing_collected_takes_no_decay(dev):
+    c = Cache(dev, 1, 1, 1, 64, 64, [40], 311)
+    q, kn, vn = inputs(1, 1, 2, 1, 3, 64, [3], 312)
+    _, lse = attention_call(dev, c, q.cuda(), kn.cuda(), vn.cuda(), None)
+    one, two = (dev.guarded((1, 1, 1, 64), torch.float32, 0.0) for _ in range(2))
+    accumulate(dev, c, q.cuda(), lse, None, None, 0.5, one)
+    accumulate(dev, c, q.cuda(), lse, None, None, math.inf, two)
+    assert dev.status() == 0 and torch.equal(one, two) and bool((one[..., :40] > 0).all())
