@@ -12,6 +12,10 @@
  *   dlm_guided_accept        longest agreeing prefix between the DLM proposals and an
  *                            autoregressive guider's argmax                 (Algorithm 1)
  *
+ * and, beyond the paper, a cache that holds more sequences: dlm_kv_cache_commit_q4, dlm_freecache_attn_step_q4 and
+ * dlm_kv_cache_read_q4 keep it in 4 bits a value; dlm_cache_weight_accumulate and dlm_kv_cache_evict (and their _q4 forms) find
+ * the rows that attention looks at and let the others go.
+ *
  * Conventions
  *   - Every function returns an int: DLM_OK (0) or a negative DLM_ERR_* code.  When an
  *     argument error is returned nothing has been launched.
@@ -82,7 +86,7 @@ int64_t dlm_launch_count(const dlm_ctx* ctx);
  * how the give-up path of every wait in the kernels is exercised without hanging a GPU. */
 int dlm_selftest_wait_timeout(dlm_ctx* ctx, uint64_t limit_ns, void* stream);
 
-/* Diagnostic: sets the limit of the attention kernel's device-side waits on work still to come (TMA copies, MMAs,
+/* Diagnostic: sets the limit of the attention kernels' (dlm_freecache_attn_step, dlm_freecache_attn_step_q4) device-side waits on work still to come (TMA copies, MMAs,
  * other blocks' partial results) for the calls that follow.  Two values are compiled in: 2 000 000 000 (2 s, the
  * default) and 0; anything else up to 2 s is DLM_ERR_UNSUPPORTED, anything above DLM_ERR_SHAPE.
  * 0 means "do not wait at all": the first wait whose data has not arrived yet gives up, every role of the block

@@ -10,6 +10,9 @@
 // score, and the sums and O^T are moved to it).  A first score that is not finite is no reference: the lowest number stands in for it, which any
 // finite score then replaces.  Sums are per thread and added up once, at the end of the segment, in a fixed order.
 //
+// 8 sequences of 1 to 4001 rows, 32 heads, one query row each: 71 us, 1.9 TB/s of the cache, bound by decoding (98 us with query rows as the
+// products' rows and two chains, 192 with one).  For 64 query rows the same form takes 781 us where two chains take 750, and for one small layer 19 instead of 8.6.
+//
 // Steps ("tiles") of 128 keys, dealt in turn to two groups of four warps, each with an O^T, references and sums of its own.  Block = 28 warps:
 //   warps 0-3, 4-7    the groups
 //   warps 8-23        decoders: K of even tiles (counted over the block's life), K of odd ones, V of even, V of odd; one lane of each has fresh

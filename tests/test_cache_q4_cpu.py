@@ -181,3 +181,16 @@ def test_reference_eviction_by_hand():
     assert out[0, 0, 0, :7].tolist() == [5.0, 9.0, 4.0, 2.0, 0.0, 0.0, 0.0] and bool(out[0, 0, 0, 7].isnan())
     kept, _ = ref.evict(torch.ones(1, 1, 1, 8), [8], 3, 0, 0)      # ties to the lowest rows
     assert kept[0, 0, 0].tolist() == [0, 1, 2]
+
+
+def test_build_checks_the_register_counts_of_the_attention_over_4_bits():
+    """Their register splits balance only at the counts that they are launched with: the build refuses any other."""
+    from paper_2505_21467_b200 import build as b
+    entry = "ptxas info    : Compiling entry function '_ZN3foo{}EEv' for 'sm_100a'\nptxas info    : Used {} registers\n"
+    log = "".join(entry.format(part, regs) for part, regs in b.Q4_ATTENTION_REGISTERS.items())
+    b.check_q4_attention_registers(log)
+    for part, regs in b.Q4_ATTENTION_REGISTERS.items():
+        with pytest.raises(RuntimeError):
+            b.check_q4_attention_registers(log.replace(entry.format(part, regs), entry.format(part, regs - 8)))
+        with pytest.raises(RuntimeError):
+            b.check_q4_attention_registers(log.replace(entry.format(part, regs), ""))
