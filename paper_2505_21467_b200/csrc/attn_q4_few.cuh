@@ -99,7 +99,7 @@ q4_attention_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
   uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(flags + 2);
   volatile int* const any_empty = flags + 3;
   volatile uint32_t* const too_large = reinterpret_cast<volatile uint32_t*>(flags + 4);   // [group]: the group's last tile (counted from 1) with such a score
-  const Lengths len(flags + kFlagBytes / 4, p.batch);
+  const Lengths len(flags + kFlagBytes / 4, p.batch, p.all_lengths);
 
   const uint32_t bar_q_full = sm_bar, bar_q_empty = sm_bar + 8, bar_drain = sm_bar + 16, bar_fold = sm_bar + 32;   // [1], [1], [2], [3]
   const uint32_t bar_s_ready = sm_bar + 56, bar_s_empty = bar_s_ready + 32;                       // [group][buffer]

@@ -75,6 +75,7 @@ struct Params {
   int n_rc, chunk, rows, rows_pad;   // row chunks, rows of a full chunk (128 or 256), rows of a unit, those in whole warps
   int fresh_box;    // rows of a TMA box of fresh K / V
   int min_share;
+  int all_lengths;  // few query rows: whether shared memory holds more of the lengths than the prefix
   FastDiv by_batch, by_rc, by_kv_heads, by_q_cap;
   float scale_log2;
   int* status;
@@ -107,8 +108,13 @@ __device__ __forceinline__ void find_unit(const Params& p, const Lengths& s, con
   const int grp = d.group_of(item, rest);
   g.b = element_of(s, p.batch, rest);
   g.layer = p.by_kv_heads.divmod(p.by_rc.divmod(grp, g.rc), g.kvh);
-  g.Lc = s.lc[g.b];
-  g.Lq = s.lq[g.b];
+  if (kKeys == kStep || s.lc) {
+    g.Lc = s.lc[g.b];
+    g.Lq = s.lq[g.b];
+  } else {
+    g.Lc = max(0, min(p.cache_len[g.b], p.capacity));
+    g.Lq = p.q_len ? max(0, min(p.q_len[g.b], p.q_cap)) : p.q_cap;
+  }
   g.n_c = (g.Lc + kKeys - 1) / kKeys;
   g.unit_begin = grp * d.sum + s.prefix[g.b];
 }
@@ -700,9 +706,13 @@ extern "C" int dlm_freecache_attn_step_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* c
     DLM_CUDA_TRY(cudaFuncSetAttribute(reinterpret_cast<const void*>(kern), cudaFuncAttributeMaxDynamicSharedMemorySize, limit));
     ctx->q4_smem_limit[which] = limit;
   }
-  const int smem = 1024 + (D == 128 ? tile_bytes<128>(kind) : tile_bytes<64>(kind)) + kBarrierBytes + kFlagBytes + 4 * length_ints(cache->batch);
+  const int without_lengths = 1024 + (D == 128 ? tile_bytes<128>(kind) : tile_bytes<64>(kind)) + kBarrierBytes + kFlagBytes;
+  // (heads of 128, few query rows: there is room for all lengths of 399 sequences, for the prefix alone of 1024)
+  const bool all_lengths = !is_few || without_lengths + 4 * length_ints(cache->batch) <= ctx->q4_smem_limit[which];
+  const int smem = without_lengths + 4 * length_ints(cache->batch, all_lengths);
   if (smem > ctx->q4_smem_limit[which]) return DLM_ERR_UNSUPPORTED;
   Params p;
+  p.all_lengths = all_lengths;
   p.n_rc = n_rc;
   p.cache_len = cache->cache_len;
   p.q_len = q_len;

@@ -9,11 +9,12 @@ namespace {
 
 struct Lengths {   // in shared memory, by batch element
   int* prefix;     // [batch + 1] steps of the elements before
-  int* lc;         // [batch] cached rows
+  int* lc;         // [batch] cached rows; NULL: not kept (no room), whoever needs them reads them again
   int* lq;         // [batch] active rows
-  __device__ __forceinline__ Lengths(int* at, int batch) : prefix(at), lc(at + batch + 1), lq(at + 2 * batch + 1) {}
+  __device__ __forceinline__ Lengths(int* at, int batch, bool all = true)
+      : prefix(at), lc(all ? at + batch + 1 : nullptr), lq(all ? at + 2 * batch + 1 : nullptr) {}
 };
-inline int length_ints(int batch) { return 3 * batch + 1; }
+inline int length_ints(int batch, bool all = true) { return all ? 3 * batch + 1 : batch + 1; }
 
 // One warp: lengths (clamped, and recorded where out of range) and the prefix of steps_of(cached rows, active rows).
 template <typename Steps>
@@ -32,8 +33,10 @@ __device__ __forceinline__ void read_lengths(const int32_t* cache_len, const int
         Lq = max(0, min(Lq, q_cap));
       }
       steps = steps_of(Lc, Lq);
-      s.lc[b] = Lc;
-      s.lq[b] = Lq;
+      if (s.lc) {
+        s.lc[b] = Lc;
+        s.lq[b] = Lq;
+      }
     }
     int inc = steps;
 #pragma unroll

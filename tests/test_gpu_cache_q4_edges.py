@@ -315,3 +315,40 @@ def test_nothing_collected_takes_no_decay(dev):
     accumulate(dev, c, q.cuda(), lse, None, None, 0.5, one)
     accumulate(dev, c, q.cuda(), lse, None, None, math.inf, two)
     assert dev.status() == 0 and torch.equal(one, two) and bool((one[..., :40] > 0).all())
+
+
+@pytest.mark.parametrize("D,g,L", [(128, 17, 1), (128, 1, 2), (128, 3, 12), (128, 1, 130), (64, 32, 1)])
+def test_the_largest_batch(dev, D, g, L):
+    """1024 sequences, whose lengths take what shared memory a kernel has left."""
+    B = 1024
+    lens, lq = [(7 * b) % 24 for b in range(B)], [(b % (L + 1)) if b % 3 else L for b in range(B)]
+    c = Cache(dev, 1, B, 1, 24, D, lens, 321)
+    q, kn, vn = inputs(1, B, g, 1, L, D, lq, 322)
+    q_len = torch.tensor(lq, dtype=torch.int32, device="cuda")
+    out, lse = attention_call(dev, c, q.cuda(), kn.cuda(), vn.cuda(), q_len)
+    assert dev.status() == 0
+    check_attention(c, q, kn, vn, lq, out, lse)
+    weight = dev.guarded((1, B, 1, 24), torch.float32, 0.0)
+    accumulate(dev, c, q.cuda(), lse, q_len, None, 0.0, weight)
+    assert dev.status() == 0
+    want, most = ref.weights(c.values("k", 0), lens, q[0], lse[0].cpu(), lq, None, 0.0)
+    seen = ~want.isnan()
+    rel = 2 * D * 2.0 ** -24 * most + 2.0 ** -22 * most + 2.0 ** -20 + g * L * 2.0 ** -24
+    assert bool(((weight[0].cpu().double() - want).abs() <= rel * want + 2.0 ** -120)[seen].all())
+
+
+def test_a_length_out_of_range_in_the_largest_batch(dev):
+    """... is clamped and reported there too."""
+    B, D = 1024, 128
+    c = Cache(dev, 1, B, 1, 24, D, [10] * B, 331)
+    q, kn, vn = inputs(1, B, 20, 1, 1, D, [1] * B, 332)
+    out, lse = attention_call(dev, c, q.cuda(), kn.cuda(), vn.cuda(), None)
+    assert dev.status() == 0
+    for wrong, same in ((1 << 30, 24), (-3, 0)):
+        c.cache_len[500] = same
+        want, w_lse = attention_call(dev, c, q.cuda(), kn.cuda(), vn.cuda(), None)
+        assert dev.status() == 0
+        c.cache_len[500] = wrong
+        got, g_lse = attention_call(dev, c, q.cuda(), kn.cuda(), vn.cuda(), None)
+        assert dev.status() == dlm.DLM_ERR_CAPACITY
+        assert torch.equal(got, want) and torch.equal(g_lse, w_lse)
