@@ -473,7 +473,8 @@ int dlm_kv_cache_read_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* cache, const int32
                          int n_max, int layer_begin, int layer_end, void* k_out, void* v_out, void* stream);
 
 /* dlm_freecache_attn_step_q4 — dlm_freecache_attn_step over a 4-bit cache: keys and values are the cache's values and the fresh bf16
- * rows.  Arguments, results, limits and data-dependent behaviour as there (cache_len_hint: how many blocks to launch; a poor one costs speed,
+ * rows.  Arguments, results and data-dependent behaviour as there; at most 1024
+ * sequences and 2^20 query rows a KV head (cache_len_hint: how many blocks to launch; a poor one costs speed,
  * never correctness); the workspace is dlm_attn_workspace_bytes_q4's, 256-byte aligned.  Keys whose score is -infinity or below -2^30 have no weight beside
  * any other; a query row whose every score (times log2 e) is beyond 2^29 in magnitude, where fp32 scores are tens of units apart, has no defined
  * result. */
@@ -492,10 +493,12 @@ int dlm_freecache_attn_step_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* cache, int l
  * sums in fp32.
  *   q         device, bf16 [layers][batch][n_q_heads][q_cap][head_dim], the step's queries;  lse device, fp32 [layers][batch][n_q_heads][q_cap]
  *   collected device, fp32 [n_layers][batch][n_kv_heads][capacity] (all layers of the cache), or NULL: nothing yet.  It may be `weight`.
- *             Not read where decay is 0.
+ *             Not read where decay is 0.  A row committed since the last call starts from what its place holds: 0 in an array that was
+ *             cleared at the start and that dlm_kv_cache_evict's weight_out was.
  *   weight    device, fp32 [n_layers][batch][n_kv_heads][capacity]; rows at or beyond cache_len[b], and other layers, are left as they were
  *   other arguments as dlm_freecache_attn_step.  A NaN decay is DLM_ERR_UNSUPPORTED.
- * Supported: head_dim in {64, 128}; n_q_heads a multiple of n_kv_heads; q_cap <= 4096; 16-byte aligned q and cache.
+ * Supported: head_dim in {64, 128}; n_q_heads a multiple of n_kv_heads; q_cap <= 4096; (n_q_heads / n_kv_heads) * q_cap <= 2^20; at most 1024
+ * sequences; 16-byte aligned q and cache.
  * Data-dependent: lengths out of range are clamped and recorded as DLM_ERR_CAPACITY; an expired device wait as DLM_ERR_TIMEOUT.
  */
 int dlm_cache_weight_accumulate(dlm_ctx* ctx, const dlm_kv_cache* cache, int layer_begin, int layer_end, const void* q,
