@@ -6,6 +6,9 @@
 // its sum over the query rows runs along the columns of that lane, in registers and in a fixed order, with no exchange between threads and
 // no atomics.  Per (key, query) the tensor pipe needs 2 D flops and the thread one fused multiply-add, an exponential and an addition.
 //
+// Query rows that take no part are zeros with a logarithm far below all others, so their terms are 2^(0 - 3e38) = 0 with no test of any column.  A
+// key that is not finite (bf16 cache) makes 0 * inf = NaN of them; a key whose sum is NaN is therefore summed once more without those columns.
+//
 // A step is a tile of 128 keys of a (layer, batch element, KV head) against 128 query rows; a tile meets all query rows of its KV head.
 // Block = 32 warps (24 without decoders), one block per SM with a contiguous share of the tiles, dealt to four groups in turn.  What bounds a group
 // is latency: a tile takes it a chain of waits, decoding, products, loads from TMEM and sums of 2000 - 4000 cycles, hence four of them.
@@ -51,6 +54,7 @@ struct Shape {
 };
 constexpr int kMaxPacked = 8;                        // packed K tiles: as many as there is room for
 constexpr int kLogBytes = 2 * kRows * 4;
+constexpr float kLeftOut = -3.402823466e38f;         // in place of minus the logarithm of a query row that takes no part
 
 struct Params {
   const int32_t* cache_len;
@@ -109,6 +113,27 @@ struct Ring {   // the next use of a ring of n stages: which stage, and the pari
     }
   }
 };
+
+// The sum over n16 query rows (columns of TMEM from `from` on, logarithms at log_at) without those that take no part; what they hold is not
+// looked at.  The others' terms are added in the same order as in the kernel, so a sum that is a number comes out with the same bits.
+__device__ __noinline__ float sum_of_those_that_take_part(uint32_t from, uint32_t log_at, int n16, float scale_log2) {
+  float a[4] = {};
+#pragma unroll 1
+  for (int i0 = 0; i0 < n16; i0 += 16) {
+    uint32_t v[16];
+    tmem_ld16(from + i0, v);
+    tmem_ld_wait();
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const float4 l = ld_shared_f4(log_at + (i0 + i) * 4);
+      const float minus_log[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (minus_log[c] != kLeftOut) a[c] += ex2_approx(fmaf(__uint_as_float(v[i + c]), scale_log2, minus_log[c]));
+    }
+  }
+  return (a[0] + a[1]) + (a[2] + a[3]);
+}
 
 // Tiles begin + w, begin + w + 4, .. of a segment belong to group w of the warps.  Every role enumerates the loads of query rows alike: events,
 // event e in slot e & 1.  Up to two chunks: one event each for a segment; more: one each for four tiles.
@@ -323,8 +348,8 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 #pragma unroll
         for (int j = 0; j < kRows / 32; ++j) {
           const int r = j * 32 + lane;
-          logs[s * kRows + r] = out[j] ? -CUDART_INF_F : x[j] * -1.4426950408889634f;
-          // a row that takes no part: 0 * scale - inf, whatever it holds
+          logs[s * kRows + r] = out[j] ? kLeftOut : x[j] * -1.4426950408889634f;
+          // a row that takes no part: zeros, whatever it holds
           for (uint32_t todo = __ballot_sync(0xffffffffu, out[j] && r < n16); todo != 0; todo &= todo - 1)
             if (lane < D / 8) q4::clear_piece<D>(sm_q + s * q_slot, p.q_panel, (j * 32 + __ffs(todo) - 1) * (D / 8) + lane);
         }
@@ -382,7 +407,7 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       for (int t0 = g.begin; t0 < g.end && ok; t0 += kGroupsOfTiles) {
         const int t = t0 + w;
         if (t < g.end) {
-          uint64_t a01 = 0, a23 = 0;   // pairs of sums
+          float total = 0.f;
           const int j = t * kKeys + key;
           const float before = ahead;
           ahead = collected_of(t + kGroupsOfTiles);
@@ -394,6 +419,7 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             if (!ok) break;
             tc_fence_after_sync();
             const uint32_t from = t_s + b * buf_cols, log_at = sm_log + (e & 1) * kRows * 4;
+            uint64_t a01 = 0, a23 = 0;   // pairs of sums
             auto add = [&](const uint32_t* v, int i0, int n) {
 #pragma unroll
               for (int i = 0; i < 32; i += 4) {
@@ -419,6 +445,12 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
               tmem_ld_wait();
               add(v, i, 16);
             }
+            float a0, a1, a2, a3;
+            unpack2(a01, a0, a1);
+            unpack2(a23, a2, a3);
+            float sum = (a0 + a1) + (a2 + a3);
+            if (!kQ4 && __any_sync(0xffffffffu, sum != sum)) sum = sum_of_those_that_take_part(from, log_at, n16, p.scale_log2);   // rare
+            total += sum;
             __syncwarp();
             if (lane == 0) {
               tc_fence_before_sync();
@@ -427,10 +459,7 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             }
           }
           if (!ok) break;
-          float a0, a1, a2, a3;
-          unpack2(a01, a0, a1);
-          unpack2(a23, a2, a3);
-          if (j < g.Lc) p.weight[row0 + j] = fmaf(p.decay, before, (a0 + a1) + (a2 + a3));
+          if (j < g.Lc) p.weight[row0 + j] = fmaf(p.decay, before, total);
         } else if (!resident) {   // no tile for the group: the query rows are not needed here
           for (int c = 0; c < p.n_qc && ok; ++c) {
             ok = mbar_wait_warp(bar_q_ready + 8 * ((ev + c) & 1), ((ev + c) >> 1) & 1, abort_ptr);
