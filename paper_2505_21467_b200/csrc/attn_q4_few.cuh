@@ -474,6 +474,7 @@ q4_attention_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             }
           }
           if (n_own > n_first) {                                   // the group's products so far are complete (pv_done above)
+            tc_fence_after_sync();
             const uint32_t t_o = tmem + t_lane + G::kColO + w * 64;
 #pragma unroll 1
             for (int c = 0; c < N; c += 16) {
@@ -521,10 +522,15 @@ q4_attention_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
         float* const to = sums + (w * 4 + (warp & 3)) * N + column_of<N>(lane);
         to[0] = l[0];
       }
+      // (fences on both sides: behind it a group reads the other's O^T, of whose products only that group has waited for; and the last one lets
+      // the next segment's products overwrite what both have read)
       auto meet = [&](int i) {
+        tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_fold + 8 * i);
-        return wait(bar_fold + 8 * i, seg & 1);
+        if (!wait(bar_fold + 8 * i, seg & 1)) return false;
+        tc_fence_after_sync();
+        return true;
       };
       ok = meet(0);
       if (!ok) break;
@@ -575,7 +581,6 @@ q4_attention_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
           }
         }
       }
-      tc_fence_before_sync();
       ok = meet(2);                                                // O^T, the references and sums have been read
       ++seg;
     }

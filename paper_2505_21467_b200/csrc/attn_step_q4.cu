@@ -536,6 +536,7 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           __syncwarp();
           if (lane == 0) mbar_arrive(bar_fold + 8);
           ok = wait(bar_fold + 8, seg & 1);
+          tc_fence_after_sync();
         }
         ++seg;
       }
