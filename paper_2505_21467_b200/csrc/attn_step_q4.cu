@@ -19,7 +19,7 @@
 // workspace.  A second, small launch joins the parts in block order (the result does not depend on timing), so that no block waits for
 // another.
 //
-// One layer of 32 x 7 query rows over 1024 cached ones: 15.3 us (20.5 in the first form, 17.5 before the joining launch looked for its
+// One layer of 32 x 7 query rows over 1024 cached ones: 15.9 us (20.5 in the first form, 17.5 before the joining launch looked for its
 // parts early; shares of at least 1, 2, 3, 4 and 6 steps took 18.9, 19.0, 19.7, 20.3 and 22.9 in between).  28 layers over 16301 rows: 267 us, 0.48 of the tensor peak, the softmax warps' chain: per step 1470
 // of 2236 cycles.  32 layers x 4 x 32 heads over 2048 rows, 64 query rows (half of the M tile): 750 us, 1.9 TB/s of the cache; 49 % of the issue
 // slots and 34 % of the tensor pipe are in use, and without any decoding, exponentials or products the waits alone took 490.  (16 decoding warps for
@@ -556,72 +556,94 @@ q4_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 
 // Joins the parts of split units.  Every boundary between two shares that lies inside a unit belongs to that unit; the first of them does
 // the work for all its parts.  Block = (boundary, 32 rows); a warp has 8 columns, a lane a row.
+//
+// What is to be joined follows from the lengths, and is found while the parts are still computed (one layer: 17.5 us without this).  Nothing
+// promises that lengths read before the wait are those that the attention kernel read, so they are read again behind it, next to the parts; where
+// any differs, everything is done once more with the new ones.  Until then no result is stored, and parts are only read within the workspace:
+// lengths are clamped, so any give slots of this grid.
 template <int D, bool kFew>
 __global__ void __launch_bounds__(D * 4, 2) q4_attention_join_kernel(const __grid_constant__ Params p, int grid) {
   extern __shared__ int join_smem[];
   const Lengths len(join_smem, p.batch);
   constexpr int kKeys = kFew ? few::kKeys : kStep;
-  // The lengths are not written by the attention kernel, and this one starts only when every block of that has waited for those before:
-  // what is to be joined is found while its parts are still computed.
-  if (threadIdx.x < 32) read_lengths<kKeys>(p, len, nullptr);
-  __syncthreads();
-  const Deal d = deal_of(p, len, grid);
-  const int c = blockIdx.x + 1;
-  bool joins = c < d.n;
-  Segment g = {};
-  int c_first = 0, c_last = 0, first_slot = 0;
-  if (joins) {
-    const int boundary = d.lo(c);
-    find_unit<kKeys>(p, len, d, boundary, g);
-    joins = g.unit_begin != boundary && d.lo(c - 1) <= g.unit_begin;   // inside a unit, and its first
-    const int unit_end = g.unit_begin + len.prefix[g.b + 1] - len.prefix[g.b];
-    c_first = c - 1;
-    c_last = d.owner(unit_end - 1);
-    // the part of block b: its first segment if the part starts where its share does, as all but the first part do, else its second
-    first_slot = 2 * c_first + (d.lo(c_first) >= g.unit_begin ? 0 : 1);
-  }
-  dlm_grid_dependency_wait();
-  dlm_trigger_dependents();
-  if (!joins) return;
-  const int row = blockIdx.y * 32 + (threadIdx.x & 31), c8 = threadIdx.x >> 5;
-  const int r_kv = g.rc * p.chunk + row;
-  if (row >= p.rows || r_kv >= p.rows_total) return;
-  const bool active = r_kv - p.by_q_cap.div(r_kv) * p.q_cap < g.Lq;
-  const size_t out = (((size_t)g.layer * p.batch + g.b) * p.n_q_heads + (size_t)g.kvh * p.group) * p.q_cap + r_kv;
   constexpr int kAtOnce = 4;
-  float m = -CUDART_INF_F, l = 0.f, o[8] = {};
+  const int row = blockIdx.y * 32 + (threadIdx.x & 31), c8 = threadIdx.x >> 5, c = blockIdx.x + 1;
+  bool joins;      // the block has a unit to join, and this thread a row of it
+  Segment g = {};
+  float m, l, o[8];
 #pragma unroll 1
-  for (int b0 = c_first; b0 <= c_last; b0 += kAtOnce) {
-    float2 ml[kAtOnce];
-    float4 x[kAtOnce], y[kAtOnce];
-#pragma unroll
-    for (int j = 0; j < kAtOnce; ++j) {
-      ml[j] = make_float2(-CUDART_INF_F, 0.f);
-      x[j] = y[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (b0 + j <= c_last) {
-        const size_t s = (size_t)(b0 + j == c_first ? first_slot : 2 * (b0 + j));
-        const float4* po = kFew ? p.ws_o + (s * p.rows_pad + row) * (D / 4) + 2 * c8 : p.ws_o + (s * (D / 4) + 2 * c8) * p.rows_pad + row;
-        ml[j] = __ldcg(p.ws_ml + s * p.rows_pad + row);
-        x[j] = __ldcg(po);
-        y[j] = __ldcg(po + (kFew ? 1 : p.rows_pad));
+  for (bool early = true;; early = false) {
+    if (threadIdx.x < 32) read_lengths(p.cache_len, p.q_len, p.batch, p.capacity, p.q_cap, nullptr, len, nullptr, steps_of<kKeys>);   // (recorded by the kernel before)
+    __syncthreads();
+    const Deal d = deal_of(p, len, grid);
+    joins = c < d.n;
+    int c_first = 0, c_last = 0, first_slot = 0;
+    if (joins) {
+      const int boundary = d.lo(c);
+      find_unit<kKeys>(p, len, d, boundary, g);
+      joins = g.unit_begin != boundary && d.lo(c - 1) <= g.unit_begin;   // inside a unit, and its first
+      const int unit_end = g.unit_begin + len.prefix[g.b + 1] - len.prefix[g.b];
+      c_first = c - 1;
+      c_last = d.owner(unit_end - 1);
+      // the part of block b: its first segment if the part starts where its share does, as all but the first part do, else its second
+      first_slot = 2 * c_first + (d.lo(c_first) >= g.unit_begin ? 0 : 1);
+    }
+    joins = joins && row < p.rows && g.rc * p.chunk + row < p.rows_total;
+    int now_c = 0, now_q = 0;
+    if (early) {
+      dlm_grid_dependency_wait();
+      dlm_trigger_dependents();
+      if (threadIdx.x < p.batch) {
+        now_c = clamped_length(p.cache_len, threadIdx.x, p.capacity);
+        now_q = clamped_length(p.q_len, threadIdx.x, p.q_cap);
       }
     }
-    float m_new = m;
+    m = -CUDART_INF_F;
+    l = 0.f;
 #pragma unroll
-    for (int j = 0; j < kAtOnce; ++j) m_new = fmaxf(m_new, ml[j].x);
-    const float old = ex2_approx(m - m_new);   // the first time 2^-inf = 0
-    l *= old;
+    for (int i = 0; i < 8; ++i) o[i] = 0.f;
+#pragma unroll 1
+    for (int b0 = c_first; joins && b0 <= c_last; b0 += kAtOnce) {
+      float2 ml[kAtOnce];
+      float4 x[kAtOnce], y[kAtOnce];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] *= old;
+      for (int j = 0; j < kAtOnce; ++j) {
+        ml[j] = make_float2(-CUDART_INF_F, 0.f);
+        x[j] = y[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (b0 + j <= c_last) {
+          const size_t s = (size_t)(b0 + j == c_first ? first_slot : 2 * (b0 + j));
+          const float4* po = kFew ? p.ws_o + (s * p.rows_pad + row) * (D / 4) + 2 * c8 : p.ws_o + (s * (D / 4) + 2 * c8) * p.rows_pad + row;
+          ml[j] = __ldcg(p.ws_ml + s * p.rows_pad + row);
+          x[j] = __ldcg(po);
+          y[j] = __ldcg(po + (kFew ? 1 : p.rows_pad));
+        }
+      }
+      float m_new = m;
 #pragma unroll
-    for (int j = 0; j < kAtOnce; ++j) {
-      const float w = ex2_approx(ml[j].x - m_new);
-      l = fmaf(w, ml[j].y, l);
-      o[0] = fmaf(w, x[j].x, o[0]); o[1] = fmaf(w, x[j].y, o[1]); o[2] = fmaf(w, x[j].z, o[2]); o[3] = fmaf(w, x[j].w, o[3]);
-      o[4] = fmaf(w, y[j].x, o[4]); o[5] = fmaf(w, y[j].y, o[5]); o[6] = fmaf(w, y[j].z, o[6]); o[7] = fmaf(w, y[j].w, o[7]);
+      for (int j = 0; j < kAtOnce; ++j) m_new = fmaxf(m_new, ml[j].x);
+      const float old = ex2_approx(m - m_new);   // the first time 2^-inf = 0
+      l *= old;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] *= old;
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) {
+        const float w = ex2_approx(ml[j].x - m_new);
+        l = fmaf(w, ml[j].y, l);
+        o[0] = fmaf(w, x[j].x, o[0]); o[1] = fmaf(w, x[j].y, o[1]); o[2] = fmaf(w, x[j].z, o[2]); o[3] = fmaf(w, x[j].w, o[3]);
+        o[4] = fmaf(w, y[j].x, o[4]); o[5] = fmaf(w, y[j].y, o[5]); o[6] = fmaf(w, y[j].z, o[6]); o[7] = fmaf(w, y[j].w, o[7]);
+      }
+      m = m_new;
     }
-    m = m_new;
+    if (!early) break;
+    bool changed = threadIdx.x < p.batch && (now_c != len.lc[threadIdx.x] || now_q != len.lq[threadIdx.x]);
+    for (int b = threadIdx.x + D * 4; b < p.batch; b += D * 4)
+      changed |= clamped_length(p.cache_len, b, p.capacity) != len.lc[b] || clamped_length(p.q_len, b, p.q_cap) != len.lq[b];
+    if (!__syncthreads_or(changed)) break;
   }
+  if (!joins) return;
+  const int r_kv = g.rc * p.chunk + row;
+  const bool active = r_kv - p.by_q_cap.div(r_kv) * p.q_cap < g.Lq;
+  const size_t out = (((size_t)g.layer * p.batch + g.b) * p.n_q_heads + (size_t)g.kvh * p.group) * p.q_cap + r_kv;
   const float inv = 1.f / l;
   uint32_t h[4];
 #pragma unroll

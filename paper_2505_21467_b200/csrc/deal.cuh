@@ -16,7 +16,9 @@ struct Lengths {   // in shared memory, by batch element
 };
 inline int length_ints(int batch, bool all = true) { return all ? 3 * batch + 1 : batch + 1; }
 
-// One warp: lengths (clamped, and recorded where out of range) and the prefix of steps_of(cached rows, active rows).
+__device__ __forceinline__ int clamped_length(const int32_t* len, int b, int most) { return len ? max(0, min(__ldcg(len + b), most)) : most; }
+
+// One warp: lengths (clamped, and recorded where out of range, unless `status` is NULL) and the prefix of steps_of(cached rows, active rows).
 template <typename Steps>
 __device__ __forceinline__ void read_lengths(const int32_t* cache_len, const int32_t* q_len, int batch, int capacity, int q_cap, int* status,
                                              const Lengths& s, volatile int* any_empty, Steps steps_of) {
@@ -26,9 +28,9 @@ __device__ __forceinline__ void read_lengths(const int32_t* cache_len, const int
     const int b = b0 + lane;
     int steps = 0;
     if (b < batch) {
-      int Lc = cache_len[b], Lq = q_len ? q_len[b] : q_cap;
+      int Lc = __ldcg(cache_len + b), Lq = q_len ? __ldcg(q_len + b) : q_cap;
       if (Lc < 0 || Lc > capacity || Lq < 0 || Lq > q_cap) {
-        dlm_set_status(status, DLM_ERR_CAPACITY);
+        if (status) dlm_set_status(status, DLM_ERR_CAPACITY);
         Lc = max(0, min(Lc, capacity));
         Lq = max(0, min(Lq, q_cap));
       }
