@@ -86,8 +86,9 @@ int64_t dlm_launch_count(const dlm_ctx* ctx);
  * how the give-up path of every wait in the kernels is exercised without hanging a GPU. */
 int dlm_selftest_wait_timeout(dlm_ctx* ctx, uint64_t limit_ns, void* stream);
 
-/* Diagnostic: sets the limit of the attention kernels' (dlm_freecache_attn_step, dlm_freecache_attn_step_q4) device-side waits on work still to come (TMA copies, MMAs,
- * other blocks' partial results) for the calls that follow.  Two values are compiled in: 2 000 000 000 (2 s, the
+/* Diagnostic: sets the limit of the device-side waits on work still to come (TMA copies, MMAs, other blocks' partial
+ * results) of dlm_freecache_attn_step, dlm_freecache_attn_step_q4, dlm_cache_weight_accumulate and
+ * dlm_cache_weight_accumulate_q4 for the calls that follow.  Two values are compiled in: 2 000 000 000 (2 s, the
  * default) and 0; anything else up to 2 s is DLM_ERR_UNSUPPORTED, anything above DLM_ERR_SHAPE.
  * 0 means "do not wait at all": the first wait whose data has not arrived yet gives up, every role of the block
  * unwinds (copies and MMAs already issued are still waited for, with the 2 s limit, before the block releases its

@@ -141,12 +141,15 @@ __device__ __noinline__ float sum_of_those_that_take_part(uint32_t from, uint32_
 // A wait for a barrier's phase works only when the phase before is over, so whoever waits on a barrier either has to arrive for its next
 // phase or waits behind something that does: hence stages that belong to one group, and events that each role takes, also where it has
 // no tile.
-template <int D, bool kQ4>
+//
+// kNoWait = true is the instantiation that a test selects to run the give-up path: every wait on work still to come tests its barrier once.
+template <int D, bool kQ4, bool kNoWait>
 __global__ void __launch_bounds__(Shape<D, kQ4>::kThreads, 1)
 cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ Params p) {
   using G = Shape<D, kQ4>;
   using Pk = q4::Packed<D, kKeys>;
   constexpr int KS = G::KS, kControl = kSumWarps + G::kDecodeWarps;
+  constexpr uint64_t kLimit = kNoWait ? 0ull : kWaitLimitNs;
   const uint32_t PS = (uint32_t)p.n_packed, q_slot = G::kPanels * p.q_panel;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_pad = (1024u - (smem_u32(smem_raw) & 1023u)) & 1023u;
@@ -218,7 +221,7 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     uint32_t kt = 0, ev = 0;   // packed tiles and events so far; tiles of the groups (bf16)
     Ring ps;
     uint32_t tiles[kGroupsOfTiles] = {};
-    auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_warp(bar, parity, abort_ptr); };
+    auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_warp(bar, parity, abort_ptr, kLimit); };
     auto load_q = [&](int c) {
       const uint32_t s = ev & 1;
       if (ev >= 2 && !wait(bar_q_empty + 8 * s, ((ev >> 1) - 1) & 1)) return false;
@@ -278,7 +281,7 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     if (elect_one_sync()) {
       // ================================================================= MMA issuers, one for each group of warps
       const int w = warp - kControl - 1;
-      auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait(bar, parity, abort_ptr); };
+      auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_limit(bar, parity, abort_ptr, kLimit); };
       uint32_t kt = 0, ev = 0, st = 0;   // the group's tiles, events, the group's steps so far
       const uint64_t desc_k0 = make_smem_desc_sw128(sm_k, 16, 1024), desc_q0 = make_smem_desc_sw128(sm_q, 16, 1024);
       auto take_event = [&](uint32_t e) { return wait(bar_q_ready + 8 * (e & 1), (e >> 1) & 1); };
@@ -343,7 +346,7 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           out[j] = x[j] == -CUDART_INF_F;
         }
         // the copy into the slot shows that the slot's logarithms have been used too
-        ok = mbar_wait_warp(bar_q_tx + 8 * s, (ev >> 1) & 1, abort_ptr);
+        ok = mbar_wait_warp(bar_q_tx + 8 * s, (ev >> 1) & 1, abort_ptr, kLimit);
         if (!ok) break;
 #pragma unroll
         for (int j = 0; j < kRows / 32; ++j) {
@@ -369,7 +372,7 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       while (ok && walk.next(g)) {
         for (int t = g.begin; t < g.end && ok; ++t, ps.advance(PS)) {
           const uint32_t s = ps.stage, packed = sm_p + s * G::kPackedStage;
-          ok = mbar_wait_warp(bar_p_full + 8 * s, ps.parity, abort_ptr);
+          ok = mbar_wait_warp(bar_p_full + 8 * s, ps.parity, abort_ptr, kLimit);
           if (!ok) break;
           if (((t - g.begin) & (kGroupsOfTiles - 1)) != w) {
             __syncwarp();
@@ -377,7 +380,7 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             continue;
           }
           const uint32_t tile = sm_k + w * G::kTile;
-          if (n > 0) ok = mbar_wait_warp(bar_k_empty + 8 * w, (n - 1) & 1, abort_ptr);
+          if (n > 0) ok = mbar_wait_warp(bar_k_empty + 8 * w, (n - 1) & 1, abort_ptr, kLimit);
           if (!ok) break;
           decoder.run(packed, tile, min(kKeys, g.Lc - t * kKeys));
           ++n;
@@ -414,8 +417,8 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           for (int c = 0; c < p.n_qc && ok; ++c, ++st) {
             const uint32_t e = ev + c, b = st % n_buf, use = st / n_buf, buf = 16 * w + 8 * b;
             const int n16 = (chunk_rows(c) + 15) & ~15;
-            ok = mbar_wait_warp(bar_s_ready + buf, use & 1, abort_ptr);   // (behind q_ready, whose logarithms are read here)
-            if (ok) ok = mbar_wait_warp(bar_q_ready + 8 * (e & 1), (e >> 1) & 1, abort_ptr);
+            ok = mbar_wait_warp(bar_s_ready + buf, use & 1, abort_ptr, kLimit);   // (behind q_ready, whose logarithms are read here)
+            if (ok) ok = mbar_wait_warp(bar_q_ready + 8 * (e & 1), (e >> 1) & 1, abort_ptr, kLimit);
             if (!ok) break;
             tc_fence_after_sync();
             const uint32_t from = t_s + b * buf_cols, log_at = sm_log + (e & 1) * kRows * 4;
@@ -462,7 +465,7 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           if (j < g.Lc) p.weight[row0 + j] = fmaf(p.decay, before, total);
         } else if (!resident) {   // no tile for the group: the query rows are not needed here
           for (int c = 0; c < p.n_qc && ok; ++c) {
-            ok = mbar_wait_warp(bar_q_ready + 8 * ((ev + c) & 1), ((ev + c) >> 1) & 1, abort_ptr);
+            ok = mbar_wait_warp(bar_q_ready + 8 * ((ev + c) & 1), ((ev + c) >> 1) & 1, abort_ptr, kLimit);
             __syncwarp();
             if (ok && lane == 0) mbar_arrive(bar_q_empty + 8 * ((ev + c) & 1));
           }
@@ -471,7 +474,7 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       }
       if (resident) {
         for (int c = 0; c < p.n_qc && ok; ++c) {
-          ok = mbar_wait_warp(bar_q_ready + 8 * ((ev + c) & 1), ((ev + c) >> 1) & 1, abort_ptr);
+          ok = mbar_wait_warp(bar_q_ready + 8 * ((ev + c) & 1), ((ev + c) >> 1) & 1, abort_ptr, kLimit);
           __syncwarp();
           if (ok && lane == 0) mbar_arrive(bar_q_empty + 8 * ((ev + c) & 1));
         }
@@ -506,9 +509,11 @@ int accumulate(dlm_ctx* ctx, const Cache* cache, const uint8_t* k_scale, int lay
   const long long units = (long long)nl * cache->batch * cache->n_kv_heads, tiles = (cache->capacity + kKeys - 1) / kKeys;
   if (units * tiles >= (1LL << 30)) return DLM_ERR_UNSUPPORTED;   // items are counted in 32 bits
   DLM_DEVICE_TRY(ctx);
-  const Kernel kern = D == 128 ? cache_weight_kernel<128, kQ4> : cache_weight_kernel<64, kQ4>;
+  const bool no_wait = ctx->wait_limit_ns == 0;
+  const Kernel kern = D == 128 ? (no_wait ? cache_weight_kernel<128, kQ4, true> : cache_weight_kernel<128, kQ4, false>)
+                               : (no_wait ? cache_weight_kernel<64, kQ4, true> : cache_weight_kernel<64, kQ4, false>);
   const int threads = Shape<128, kQ4>::kThreads;
-  const int which = (D == 128 ? 0 : 1) + (kQ4 ? 2 : 0);
+  const int which = (D == 128 ? 0 : 1) + (kQ4 ? 2 : 0) + (no_wait ? 4 : 0);
   if (ctx->weight_smem_limit[which] == 0) {
     DLM_CUDA_TRY(cudaFuncSetAttribute(reinterpret_cast<const void*>(kern), cudaFuncAttributeMaxDynamicSharedMemorySize, ctx->max_smem_optin));
     ctx->weight_smem_limit[which] = ctx->max_smem_optin;

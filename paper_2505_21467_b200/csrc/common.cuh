@@ -65,7 +65,7 @@ struct dlm_ctx {
   int attn_clusters[17];        // clusters of so many attention blocks that the device runs at a time (0 = not asked yet, -1 = none)
   int attn_smem_limit[32];      // dynamic shared memory the attention kernels may use on this device (0 = not set up yet)
   int q4_smem_limit[16];         // ... those of the 4-bit cache
-  int weight_smem_limit[4];     // ... the kernels that accumulate weights
+  int weight_smem_limit[8];     // ... the kernels that accumulate weights
 };
 
 // Writes the descriptor of a bf16 tensor of `rank` dimensions (sizes, byte strides of dimensions 1 .., box), 128-byte swizzle,
