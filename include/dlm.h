@@ -476,7 +476,7 @@ int dlm_kv_cache_read_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* cache, const int32
 /* dlm_freecache_attn_step_q4 — dlm_freecache_attn_step over a 4-bit cache: keys and values are the cache's values and the fresh bf16
  * rows.  Arguments, results and data-dependent behaviour as there; at most 1024
  * sequences and 2^20 query rows a KV head (cache_len_hint: how many blocks to launch; a poor one costs speed,
- * never correctness); the workspace is dlm_attn_workspace_bytes_q4's, 256-byte aligned.  Keys whose score is -infinity or below -2^30 have no weight beside
+ * never correctness); the workspace is dlm_attn_workspace_bytes_q4's (0 for sizes that the call refuses), 256-byte aligned.  Keys whose score is -infinity or below -2^30 have no weight beside
  * any other; a query row whose every score (times log2 e) is beyond 2^29 in magnitude, where fp32 scores are tens of units apart, has no defined
  * result. */
 size_t dlm_attn_workspace_bytes_q4(const dlm_ctx* ctx, const dlm_kv_cache_q4* cache, int n_layers_in_call, int n_q_heads, int q_cap);

@@ -677,7 +677,10 @@ int tile_bytes(int kind) {
 struct Workspace {
   size_t o_bytes, ml_bytes;
 };
-int rows_of(int n_q_heads, int n_kv_heads, int q_cap) { return n_q_heads / n_kv_heads * q_cap; }
+// Whether a call of these sizes is taken: query rows are counted in 32 bits, and shared memory holds the lengths of so many sequences.
+bool sizes_taken(int n_q_heads, int n_kv_heads, int q_cap, int batch) {
+  return n_q_heads % n_kv_heads == 0 && q_cap <= kMaxQCap && (long long)(n_q_heads / n_kv_heads) * q_cap <= (1 << 20) && batch <= kMaxBatch;
+}
 Workspace workspace_of(const dlm_ctx* ctx, int head_dim, int rows_total) {
   const size_t slots = 2 * (size_t)(ctx->num_sms < kMaxGrid ? ctx->num_sms : kMaxGrid), pad = (size_t)((rows_total < 256 ? rows_total : 256) + 31) / 32 * 32;
   return {slots * pad * head_dim * sizeof(float), slots * pad * 2 * sizeof(float)};
@@ -688,9 +691,9 @@ Workspace workspace_of(const dlm_ctx* ctx, int head_dim, int rows_total) {
 extern "C" size_t dlm_attn_workspace_bytes_q4(const dlm_ctx* ctx, const dlm_kv_cache_q4* cache, int n_layers_in_call,
                                               int n_q_heads, int q_cap) {
   if (!ctx || !cache || n_layers_in_call <= 0 || n_q_heads <= 0 || q_cap <= 0 || cache->n_kv_heads <= 0 || cache->batch <= 0 ||
-      (cache->head_dim != 64 && cache->head_dim != 128) || n_q_heads % cache->n_kv_heads != 0 || q_cap > kMaxQCap)
+      (cache->head_dim != 64 && cache->head_dim != 128) || !sizes_taken(n_q_heads, cache->n_kv_heads, q_cap, cache->batch))
     return 0;
-  const Workspace w = workspace_of(ctx, cache->head_dim, rows_of(n_q_heads, cache->n_kv_heads, q_cap));
+  const Workspace w = workspace_of(ctx, cache->head_dim, n_q_heads / cache->n_kv_heads * q_cap);
   return w.o_bytes + w.ml_bytes;
 }
 
@@ -702,9 +705,8 @@ extern "C" int dlm_freecache_attn_step_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* c
   const int bad = dlm_check_q4(cache);
   if (bad != DLM_OK) return bad;
   if (n_q_heads <= 0 || q_cap <= 0 || layer_begin < 0 || layer_end > cache->n_layers || layer_begin >= layer_end) return DLM_ERR_SHAPE;
-  if (n_q_heads % cache->n_kv_heads != 0) return DLM_ERR_UNSUPPORTED;
+  if (!sizes_taken(n_q_heads, cache->n_kv_heads, q_cap, cache->batch)) return DLM_ERR_UNSUPPORTED;
   const int D = cache->head_dim, group = n_q_heads / cache->n_kv_heads, nl = layer_end - layer_begin;
-  if (q_cap > kMaxQCap || (long long)group * q_cap > (1 << 20) || cache->batch > kMaxBatch) return DLM_ERR_UNSUPPORTED;
   if (((uintptr_t)q | (uintptr_t)k_new | (uintptr_t)v_new | (uintptr_t)out) & 15) return DLM_ERR_UNSUPPORTED;
   const int rows_total = group * q_cap, kind = rows_total <= 16 ? 0 : rows_total <= 32 ? 1 : rows_total <= 128 ? 2 : 3;
   const bool is_few = kind < 2;
