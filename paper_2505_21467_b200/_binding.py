@@ -132,14 +132,14 @@ def make_kv_cache(k: torch.Tensor, v: torch.Tensor, cache_len: torch.Tensor) -> 
 def make_kv_cache_q4(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
                      cache_len: torch.Tensor) -> dlm_kv_cache_q4:
     """View of caller-owned tensors: k, v uint8 [NL,B,Hkv,Lcap,D/2]; k_scale, v_scale uint8 [NL,B,Hkv,Lcap,D/32]; cache_len int32 [B]."""
-    if k.dtype != torch.uint8 or k.shape != v.shape or k.dim() != 5:
+    if k.dtype != torch.uint8 or v.dtype != torch.uint8 or k.shape != v.shape or k.dim() != 5:
         raise TypeError("k and v must be uint8 tensors of the same 5-d shape")
     NL, B, Hkv, Lcap, half = k.shape
-    if half % 16 != 0 or k_scale.dtype != torch.uint8 or k_scale.shape != (NL, B, Hkv, Lcap, half // 16) or k_scale.shape != v_scale.shape:
+    if half % 16 != 0 or k_scale.dtype != torch.uint8 or v_scale.dtype != torch.uint8 or k_scale.shape != (NL, B, Hkv, Lcap, half // 16) or k_scale.shape != v_scale.shape:
         raise TypeError("k_scale and v_scale must be uint8 tensors with one entry per 32 values of k and v")
     if cache_len.shape != (B,):
         raise TypeError("cache_len must have shape [batch]")
-    c = dlm_kv_cache_q4(_ptr(k).value, _ptr(v).value, _ptr(k_scale).value, _ptr(v_scale, torch.uint8).value,
+    c = dlm_kv_cache_q4(_ptr(k).value, _ptr(v).value, _ptr(k_scale).value, _ptr(v_scale).value,
                         _ptr(cache_len, torch.int32).value, NL, B, Hkv, Lcap, 2 * half)
     c._keepalive = (k, v, k_scale, v_scale, cache_len)
     return c

@@ -1,7 +1,8 @@
-"""Sizes that the host turns away: the workspace of a call that the attention over a 4-bit cache refuses."""
+"""Sizes and types that the host turns away: the workspace of a call that the attention over a 4-bit cache refuses, and views of other types."""
 import ctypes
 
 import pytest
+import torch
 
 import paper_2505_21467_b200 as dlm
 from paper_2505_21467_b200 import build as _build
@@ -39,3 +40,12 @@ def test_workspace_of_calls_that_are_refused_is_zero():
                     (_cache(n_kv_heads=1), (1, 1 << 20, 4096)), (_cache(batch=1025), (1, 4, 8))):
         assert _workspace_bytes(c, *args) == 0, args
     assert _workspace_bytes(_cache(n_kv_heads=1, batch=1024), 1, 256, 4096) > 0
+
+def test_views_take_bytes_only():
+    data, scale, n = torch.zeros(1, 2, 2, 8, 32, dtype=torch.uint8), torch.zeros(1, 2, 2, 8, 2, dtype=torch.uint8), torch.zeros(2, dtype=torch.int32)
+    for v in (data.to(torch.bfloat16), data.to(torch.int8), data.float()):
+        with pytest.raises(TypeError, match="k and v must be uint8"):
+            dlm.make_kv_cache_q4(data, v, scale, scale, n)
+    for v_scale in (scale.float(), scale.to(torch.int8)):
+        with pytest.raises(TypeError, match="k_scale and v_scale must be uint8"):
+            dlm.make_kv_cache_q4(data, data, scale, v_scale, n)
