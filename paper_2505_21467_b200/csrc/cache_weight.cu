@@ -452,7 +452,7 @@ cache_weight_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             unpack2(a01, a0, a1);
             unpack2(a23, a2, a3);
             float sum = (a0 + a1) + (a2 + a3);
-            if (!kQ4 && __any_sync(0xffffffffu, sum != sum)) sum = sum_of_those_that_take_part(from, log_at, n16, p.scale_log2);   // rare
+            if (!kQ4 && __any_sync(0xffffffffu, sum != sum && j < g.Lc)) sum = sum_of_those_that_take_part(from, log_at, n16, p.scale_log2);   // rare
             total += sum;
             __syncwarp();
             if (lane == 0) {
