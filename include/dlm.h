@@ -172,7 +172,8 @@ int dlm_selftest_attn_schedule(const dlm_ctx* ctx, const dlm_kv_cache* cache, in
  * For each layer l in [layer_begin, layer_end), batch element b, query head h (KV head
  * h / (n_q_heads / n_kv_heads)) and active row i < q_len(b):
  *     keys/values = cache rows [0, cache_len[b]) of layer l, then fresh rows [0, q_len(b))
- *     out[l][b][h][i][:] = sum_j softmax_j(scale * <q_i, k_j>) v_j      (fp32 accumulate)
+ *     out[l][b][h][i][:] = sum_j softmax_j(scale * <q_i, k_j>) v_j      (fp32 accumulate; the exponentials
+ *                          are rounded to bf16 for the product with v, their sum is taken before)
  *     lse[l][b][h][i]    = log sum_j exp(scale * <q_i, k_j>)            (natural log)
  * Rows i >= q_len(b) get out = 0 and lse = -inf.  More than one layer per call is only
  * meaningful when all layers' Q/K/V exist up front (a synthetic stack); a real model calls
@@ -474,11 +475,11 @@ int dlm_kv_cache_read_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* cache, const int32
                          int n_max, int layer_begin, int layer_end, void* k_out, void* v_out, void* stream);
 
 /* dlm_freecache_attn_step_q4 — dlm_freecache_attn_step over a 4-bit cache: keys and values are the cache's values and the fresh bf16
- * rows.  Arguments, results and data-dependent behaviour as there; at most 1024
- * sequences and 2^20 query rows a KV head (cache_len_hint: how many blocks to launch; a poor one costs speed,
- * never correctness); the workspace is dlm_attn_workspace_bytes_q4's (0 for sizes that the call refuses), 256-byte aligned.  Keys whose score is -infinity or below -2^30 have no weight beside
- * any other; a query row whose every score (times log2 e) is beyond 2^29 in magnitude, where fp32 scores are tens of units apart, has no defined
- * result. */
+ * rows.  Arguments, results and data-dependent behaviour as there; at most 1024 sequences and 2^20 query rows a KV head
+ * (cache_len_hint: how many blocks to launch; a poor one costs speed, never correctness); the workspace is
+ * dlm_attn_workspace_bytes_q4's (0 for heads, query rows or batches that the call refuses), 256-byte aligned.  Keys whose score
+ * is -infinity or below -2^30 have no weight beside any other; a query row whose every score (times log2 e) is beyond 2^29 in
+ * magnitude, where fp32 scores are tens of units apart, has no defined result. */
 size_t dlm_attn_workspace_bytes_q4(const dlm_ctx* ctx, const dlm_kv_cache_q4* cache, int n_layers_in_call, int n_q_heads, int q_cap);
 int dlm_freecache_attn_step_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* cache, int layer_begin,
                                int layer_end, const void* q, const void* k_new, const void* v_new,
@@ -490,8 +491,8 @@ int dlm_freecache_attn_step_q4(dlm_ctx* ctx, const dlm_kv_cache_q4* cache, int l
  * dlm_cache_weight_accumulate, dlm_cache_weight_accumulate_q4 — how much attention each cached row gets: after an attention step,
  * for every layer l of [layer_begin, layer_end), batch element b, KV head g and cached row j < cache_len[b]
  *     weight[l][b][g][j] = decay * collected[l][b][g][j] + sum_{h of g's query heads} sum_{i < q_len(b)} exp(scale * <q_hi, k_j> - lse_hi)
- * with lse as that step wrote it (rows that are inactive there have lse = -inf and are left out here).  Products of bf16 values and
- * sums in fp32.
+ * with lse as that step wrote it (rows that are inactive there have lse = -inf and are left out here, whatever the key: a cached key with an
+ * infinity or a NaN reaches its own row's weight through the rows that take part, and no others).  Products of bf16 values and sums in fp32.
  *   q         device, bf16 [layers][batch][n_q_heads][q_cap][head_dim], the step's queries;  lse device, fp32 [layers][batch][n_q_heads][q_cap]
  *   collected device, fp32 [n_layers][batch][n_kv_heads][capacity] (all layers of the cache), or NULL: nothing yet.  It may be `weight`.
  *             Not read where decay is 0.  A row committed since the last call starts from what its place holds: 0 in an array that was

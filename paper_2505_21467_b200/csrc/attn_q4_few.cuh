@@ -10,8 +10,14 @@
 // score, and the sums and O^T are moved to it).  A first score that is not finite is no reference: the lowest number stands in for it, which any
 // finite score then replaces.  Sums are per thread and added up once, at the end of the segment, in a fixed order.
 //
-// 8 sequences of 1 to 4001 rows, 32 heads, one query row each: 71 us, 1.9 TB/s of the cache, bound by decoding (98 us with query rows as the
-// products' rows and two chains, 192 with one).  For 64 query rows the same form takes 781 us where two chains take 750, and for one small layer 19 instead of 8.6.
+// P is rounded to bf16, by at most 2^-8 of itself, since the products take it so; the sums add it unrounded.  An output is off by at most
+// 2^-8 sum p |v| from this, about what its own rounding to bf16 costs.
+//
+// 8 sequences of 3630 to 4001 rows, 32 heads, one query row each: 71 us, 1.9 TB/s of the cache, bound by decoding (98 us with query rows as the
+// products' rows and two chains, 192 with one); of 1 to 4001 rows evenly: 46 us, 1.5 TB/s.  For 64 query rows the same form takes 781 us where two chains
+// take 750, and for one small layer 19 instead of 8.6.
+// Those are scores that seldom exceed a part's first by 30.  Keys twice, 4, 8 and 32 times as large: 79, 87, 92 and 108 us; references that move in every
+// tile 154, NaN in every tile 168 (32 query rows: 90, and 131, 135, 212, 299, 305 and 317).
 //
 // Steps ("tiles") of 128 keys, dealt in turn to two groups of four warps, each with an O^T, references and sums of its own.  Block = 28 warps:
 //   warps 0-3, 4-7    the groups

@@ -79,7 +79,8 @@ __device__ __forceinline__ float row_max64(const uint32_t (&s)[64]) {
 }
 
 // P = 2^(s * scale - m) for 32 scores, packed to bf16 pairs and written to 16 TMEM columns at t_p;
-// adds to the two partial row sums.  (Variants measured in the kernel and found no faster at the
+// adds to the two partial row sums, unrounded.  (P in bf16 is what the product with V takes beside bf16 values: off by at most
+// 2^-8 of itself, an output by at most 2^-8 sum p |v|, about what rounding the output costs.)  (Variants measured in the kernel and found no faster at the
 // configs' shapes: all 32 exponentials issued before the sums, and packing by integer add and byte
 // permute instead of the conversion instruction, which shares the SFU's pipe.)
 __device__ __forceinline__ void exp32_store(const uint32_t* s, float scale_log2, float m_used, uint32_t t_p, float& l0,

@@ -1,7 +1,7 @@
 // dlm_freecache_attn_step_q4: attention of the active window over [4-bit cache rows ; fresh bf16 rows].
 //
 // The arithmetic is dlm_freecache_attn_step's: scores S = Q K^T in fp32, an online softmax with base-2 exponentials, O += P V with P in
-// bf16 and O in fp32, everything on the tensor cores with S, P and O in TMEM.  A value of the cache has 7 significant bits, so the
+// bf16 (the products' operand type; sums of P in fp32, before the rounding) and O in fp32, everything on the tensor cores with S, P and O in TMEM.  A value of the cache has 7 significant bits, so the
 // bf16 tile that the products read holds it exactly; what is quantised is what was committed, nothing on the way.
 //
 // One unit is (layer, batch element, KV head, chunk of up to 256 query rows); its keys are taken in steps of 64, first the cache's,

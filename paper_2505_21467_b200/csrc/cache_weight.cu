@@ -20,7 +20,7 @@
 // Query rows lie in two slots of 128: up to 256 stay there for all tiles of a unit, more go through for every four tiles.
 //
 // 28 layers x 4 KV heads of 16301 bf16 rows against 224 query rows: 168 us (2.9 TB/s of keys, 630 TFLOP/s; 165 without the test for NaN sums); 32 x 4 x 32 heads of 2048 4-bit rows
-// against 64: 350 us (2.0 TB/s, 400 TFLOP/s; 64 % of the issue slots, 45 % of the integer pipe: decoding; exponentials 34 % of theirs, tensor pipe
+// against 64: 343 us (2.0 TB/s, 405 TFLOP/s; 64 % of the issue slots, 45 % of the integer pipe: decoding; exponentials 34 % of theirs, tensor pipe
 // 17 %).  The latter took 368 us with two groups, and 451 with packed half tiles that belong to one group instead of a ring that all decoders read.
 #include <cuda_bf16.h>
 #include <math_constants.h>
